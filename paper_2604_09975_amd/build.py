@@ -6,7 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libckks_hip.so")
-SOURCES = ["params.hip", "ntt.hip", "keyswitch.hip", "matmul.hip", "evalops.hip", "encode.hip", "probe.hip", "client.hip"]
+SOURCES = ["params.hip", "ntt.hip", "keyswitch.hip", "matmul.hip", "evalops.hip", "encode.hip", "probe.hip", "client.hip",
+           "clear_norm.hip", "clear_cache.hip", "clear_attend.hip", "clear_logits.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-ffp-contract=off", "-Wall", "-Wno-unused-function", "-Wno-unused-value", "-Wno-unused-result"]
@@ -19,7 +20,7 @@ def _stale(out, deps):
 def build(force=False, verbose=False):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    headers += [os.path.join(os.path.dirname(HERE), "include", h) for h in ("ckks.h", "ckks_measure.h")]
+    headers += [os.path.join(os.path.dirname(HERE), "include", h) for h in ("ckks.h", "ckks_measure.h", "ckks_clear.h")]
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     objs, procs = [], []

@@ -1,0 +1,690 @@
+// Attention of a chunk of new tokens over the paged cache.
+//
+// The query heads that share a kv head are rows of one problem: row i * group + g of (sequence, kv head) is new token i, head
+// kv_head * group + g.  A wave takes 32 rows.  It computes the scores transposed, S^T = K Q^T, so that a lane holds scores of
+// one row only (row lane % 32; the two halves of the wave hold different keys): maximum and sum of the softmax stay in the
+// lane but for one exchange between the halves, and the weights come out in the order in which the next product,
+// O^T = V^T P^T, wants them.  Neither scores nor weights pass through LDS.
+//
+//   RW = 4: four waves of 32 rows share each tile of keys and values (chunks of a prompt).
+//   KW > 1: one set of 32 rows, each wave takes every KW-th tile through its own stretch of LDS, without barriers, and the
+//           waves' results are joined at the end (single tokens: the time is that of reading the cache).
+// Either may split the keys over several blocks; a second kernel then joins the blocks' results in order.
+#include <algorithm>
+#include <cmath>
+
+#include "clear_device.h"
+
+namespace ckks {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+struct AttendArgs {
+    const void *q, *k, *v;
+    void *out;
+    float *lse, *part, *part_lse;
+    i64 qs[2], os[2], ks[3], vs[3], ts;
+    const int32_t *q_start, *kv_len, *table;
+    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, group, head_dim, window, causal;
+    int32_t page_shift;  // log2 of page_size, or -1
+    u32 tiles, splits, min_tiles;
+    float c;             // scale * log2(e)
+};
+
+// One 16-deep step of a 32 x 32 product.  A lane holds 8 entries of row (column) lane % 32 of A (B), those of depth
+// 8 * (lane / 32) ..; the sum over the depth does not care in which order the entries are taken, so with 32-bit types the eight
+// steps of depth 2 pair entry j of the halves.
+__device__ __forceinline__ f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+template <class T>
+struct Frag;
+template <>
+struct Frag<float> {
+    typedef f32x8 type;
+};
+template <>
+struct Frag<f16> {
+    typedef f16x8 type;
+};
+template <>
+struct Frag<bf16> {
+    typedef bf16x8 type;
+};
+
+template <class T>
+__device__ __forceinline__ typename Frag<T>::type row_frag(const T *p) {
+    typename Frag<T>::type r;
+    __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), sizeof(r));
+    return r;
+}
+
+// Entries of column `lane % 32` of the values, keys 4h .. 4h+3 and 8 + 4h .. 8 + 4h + 3 of the 16 that begin at `v` (h = lane / 32):
+// the order in which the scores' accumulators hold a row's weights.  For 16-bit types the transposing LDS read: 16 lanes
+// read 4 rows of 16 entries, and each gets a column.
+template <class T, int STRIDE>
+__device__ __forceinline__ typename Frag<T>::type col_frag(const T *v, u32 lane) {
+    typename Frag<T>::type r;
+    if constexpr (sizeof(T) == 2) {
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const T *p = v + (4 * (lane >> 5) + ((lane & 15) >> 2)) * STRIDE + (lane & 16) + 4 * (lane & 3);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * STRIDE));
+        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        __builtin_memcpy(&r, &both, 16);
+    } else {
+        const T *p = v + 4 * (lane >> 5) * STRIDE + (lane & 31);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = p[(j < 4 ? j : j + 4) * STRIDE];
+    }
+    return r;
+}
+
+// What a tile of rows works on.
+struct RowTile {
+    u32 seq, start, n, first_row, rows;  // first token and tokens of the sequence; first row of the tile, rows in all
+    i64 kv, t0;                          // keys, position of the sequence's first new token
+    u32 tile0, n_tiles, per, n_splits;   // first key tile, key tiles, key tiles of a split, splits
+};
+
+__device__ __forceinline__ i64 row_pos(const AttendArgs &a, const RowTile &r, u32 row) { return r.t0 + row / a.group; }
+
+// Key tiles that the rows first_row .. first_row + ROWS - 1 see between them.
+template <int ROWS, int TK>
+__device__ __forceinline__ void key_range(const AttendArgs &a, RowTile &r) {
+    const i64 cap = (i64)a.table_width * a.page_size;
+    r.kv = max((i64)0, min((i64)a.kv_len[r.seq], cap));
+    r.t0 = (i64)a.kv_len[r.seq] - r.n;
+    if ((i64)a.kv_len[r.seq] > cap) r.t0 = cap - r.n;
+    const u32 last = min(r.first_row + ROWS, r.rows) - 1;
+    const i64 hi = a.causal ? min(r.kv, row_pos(a, r, last) + 1) : r.kv;
+    const i64 lo = a.window ? max((i64)0, row_pos(a, r, r.first_row) - a.window + 1) : 0;
+    r.tile0 = (u32)(lo / TK);
+    r.n_tiles = hi > lo ? (u32)((hi + TK - 1) / TK) - r.tile0 : 0;
+    r.per = max(a.min_tiles, (r.n_tiles + a.splits - 1) / a.splits);
+    r.n_splits = max(1u, (r.n_tiles + r.per - 1) / r.per);
+}
+
+// The sequence that holds tile `tile` of all sequences' tiles.  Called by whole waves.
+template <int ROWS>
+__device__ __forceinline__ bool find_tile(const AttendArgs &a, u32 tile, RowTile &r) {
+    const u32 lane = threadIdx.x & 63;
+    u32 before = 0;
+    for (u32 base = 0; base < a.n_seq; base += 64) {
+        const u32 b = base + lane;
+        int s = 0, e = 0;
+        if (b < a.n_seq) {
+            s = min(max(a.q_start[b], 0), (int)a.n_tokens);
+            e = max(min(a.q_start[b + 1], (int)a.n_tokens), s);
+        }
+        const u32 tiles = ((u32)(e - s) * a.group + ROWS - 1) / ROWS;
+        u32 sum = tiles;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const u32 up = __shfl_up(sum, o);
+            if (lane >= (u32)o) sum += up;
+        }
+        const u32 total = __shfl(sum, 63);
+        if (tile - before < total) {
+            const int at = __ffsll((unsigned long long)__ballot(sum > tile - before)) - 1;
+            r.seq = base + at;
+            r.start = __shfl(s, at);
+            r.n = __shfl(e, at) - r.start;
+            r.first_row = (tile - before - (__shfl(sum, at) - __shfl(tiles, at))) * ROWS;
+            r.rows = r.n * a.group;
+            return true;
+        }
+        before += total;
+    }
+    return false;
+}
+
+template <class T>
+__device__ __forceinline__ u32 not_finite(typename Frag<T>::type x) {
+    u32 bad = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float f = (float)x[j];
+        bad |= !(__builtin_fabsf(f) <= 3.402823466e38f);
+    }
+    return bad;
+}
+
+template <class T, int DP, int RW, int KW, int TK>
+struct AttendShape {
+    static constexpr int KS = DP + 16 / (int)sizeof(T);               // row strides in LDS: keys are read 16 bytes from each
+    static constexpr int VS = DP + (sizeof(T) == 2 ? 32 : 8);         // of 32 rows, values 64 bytes (32 entries) from each of 4:
+                                                                      // these pads spread either over the banks
+    static constexpr int TILE = TK * (KS + VS);                       // entries of a tile
+    static constexpr int BUFFERS = RW > 1 ? 2 : KW;
+    static constexpr size_t STAGE_BYTES = (size_t)TILE * BUFFERS * sizeof(T);
+    static constexpr size_t JOIN_BYTES = KW > 1 ? (size_t)KW * 32 * (DP + 2) * 4 : 0;
+    static constexpr size_t LDS = STAGE_BYTES > JOIN_BYTES ? STAGE_BYTES : JOIN_BYTES;
+};
+
+template <class T, int DP, int RW, int KW, int TK, int OCC>
+__global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a) {
+    typedef AttendShape<T, DP, RW, KW, TK> Shape;
+    typedef typename Frag<T>::type frag;
+    constexpr int KS = Shape::KS, VS = Shape::VS, ROWS = 32 * RW, SUB = TK / 32, DT = DP / 32;
+    constexpr int E = 16 / sizeof(T);                  // entries of a 16-byte piece
+    constexpr int PIECES = DP / E;                     // pieces of a row
+    constexpr int STAGERS = 64 * RW;                   // threads that fetch a tile
+    constexpr int PASS = STAGERS / PIECES;             // rows that they fetch at a time
+    constexpr int PASSES = TK / PASS;
+    __shared__ __attribute__((aligned(16))) unsigned char lds[Shape::LDS];
+
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const u32 kv_head = blockIdx.x % a.kv_heads, split = blockIdx.x / a.kv_heads % a.splits;
+    RowTile r;
+    // the last tiles of a causal chunk see the most keys: they start first
+    if (!find_tile<ROWS>(a, a.tiles - 1 - blockIdx.x / a.kv_heads / a.splits, r)) return;
+    key_range<ROWS, TK>(a, r);
+    if (split >= r.n_splits) return;
+    const u32 first = split * r.per, last = min(first + r.per, r.n_tiles);
+
+    const u32 rw = RW > 1 ? wave : 0, kw = KW > 1 ? wave : 0;
+    const u32 row0 = r.first_row + 32 * rw;
+    const bool idle = row0 >= r.rows;                  // no row of this wave exists
+    const u32 row = min(row0 + (lane & 31), r.rows - 1), token = row / a.group, head = kv_head * a.group + row % a.group;
+    const i64 pos = r.t0 + token;
+    const i64 hi = a.causal ? min(r.kv, pos + 1) : r.kv, lo = a.window ? pos - a.window + 1 : 0;  // keys lo <= j < hi are seen
+    // bounds over the wave's rows: keys that all of them see, keys that any of them sees
+    const i64 p_first = row_pos(a, r, min(row0, r.rows - 1)), p_last = row_pos(a, r, min(row0 + 31, r.rows - 1));
+    const i64 all_hi = a.causal ? min(r.kv, p_first + 1) : r.kv, any_hi = a.causal ? min(r.kv, p_last + 1) : r.kv;
+    const i64 all_lo = a.window ? p_last - a.window + 1 : 0, any_lo = a.window ? p_first - a.window + 1 : 0;
+
+    frag qf[DP / 16];
+    {
+        const T *q = (const T *)a.q + (i64)(r.start + token) * a.qs[0] + head * a.qs[1];
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            const u32 d = s * 16 + half * 8;
+            if (d < a.head_dim) {
+                __builtin_memcpy(&qf[s], q + d, 8 * sizeof(T));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) qf[s][j] = (T)0.0f;
+            }
+        }
+    }
+
+    // a lane's piece of each row that it fetches
+    const u32 stager = RW > 1 ? threadIdx.x : lane, piece = stager % PIECES, fetch_row = stager / PIECES;
+    const bool piece_ok = piece * E < a.head_dim;
+    const T *kp = (const T *)a.k + (i64)kv_head * a.ks[1] + piece * E, *vp = (const T *)a.v + (i64)kv_head * a.vs[1] + piece * E;
+    const int32_t *table = a.table + (i64)r.seq * a.ts;
+    typedef uint4 piece_t;
+    piece_t kr[PASSES], vr[PASSES];
+    int32_t page;     // of key `lane` of the tile to be fetched next (lanes below TK)
+    u32 page_row;
+    auto look_up = [&](u32 tile) {
+        const i64 j = (i64)(r.tile0 + tile) * TK + (lane & (TK - 1));
+        page = -1;
+        page_row = 0;
+        if (tile < last && j < r.kv) {
+            const u32 at = a.page_shift >= 0 ? (u32)j >> a.page_shift : (u32)j / a.page_size;
+            page_row = (u32)j - at * a.page_size;
+            page = table[at];
+            if ((u32)page >= a.n_pages) page = -1;
+        }
+    };
+    auto fetch = [&]() {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const u32 key = p * PASS + fetch_row;
+            const int32_t pg = __shfl(page, key);
+            const u32 pr = __shfl(page_row, key);
+            kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
+            if (pg >= 0 && piece_ok) {
+                __builtin_memcpy(&kr[p], kp + pg * a.ks[0] + pr * a.ks[2], 16);
+                __builtin_memcpy(&vr[p], vp + pg * a.vs[0] + pr * a.vs[2], 16);
+            }
+        }
+    };
+    auto put = [&](T *buf) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const u32 key = p * PASS + fetch_row;
+            *(piece_t *)(buf + key * KS + piece * E) = kr[p];
+            *(piece_t *)(buf + TK * KS + key * VS + piece * E) = vr[p];
+        }
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = -__builtin_inff(), l = 0.0f;  // maximum of the row's scores (kept up to 2^8, below), the lane's part of the sum
+
+    auto work = [&](u32 tile, const T *buf) {
+        const i64 j0 = (i64)(r.tile0 + tile) * TK;
+        if (idle || j0 >= any_hi || j0 + TK <= any_lo) return;
+        const bool masked = j0 + TK > all_hi || j0 < all_lo;
+        f32x16 s[SUB];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) s[u] = mma(row_frag(buf + (u * 32 + (lane & 31)) * KS + d * 16 + half * 8), qf[d], s[u]);
+        }
+        // accumulator i of the lane: key 8 (i / 4) + 4 half + i % 4
+        const int see_lo = (int)max((i64)-1, min((i64)TK, lo - j0)) - 4 * (int)half, see_hi = (int)max((i64)0, min((i64)TK, hi - j0)) - 4 * (int)half;
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int key = u * 32 + 8 * (i / 4) + i % 4;
+                    if (key < see_lo || key >= see_hi) s[u][i] = -__builtin_inff();
+                }
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        // The maximum only has to keep exp2 in range: it moves when a score passes it by 8 powers of two, and then all
+        // that was summed is scaled.
+        if (__any((top - m) * a.c > 8.0f)) {
+            const float mn = fmaxf(m, top);
+            const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - mn) * a.c);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        }
+        const float mc = m == -__builtin_inff() ? 0.0f : m * a.c;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -mc));
+                l += s[u][i];
+            }
+        const T *vb = buf + TK * KS;
+        auto weights = [&](int u, int kk) {
+            frag b;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) b[j] = (T)s[u][8 * kk + j];
+            return b;
+        };
+        if (!masked) {
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int kk = 0; kk < 2; ++kk) {
+                    const frag b = weights(u, kk);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] = mma(col_frag<T, VS>(vb + (u * 32 + kk * 16) * VS + d * 32, lane), b, o[d]);
+                }
+            return;
+        }
+        // A weight of 0 does not keep an infinity or NaN of an unseen value out of a sum.  Where a tile has one, the rows
+        // that see it are counted by further products, and only those take it in.
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                const frag b = weights(u, kk);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    frag v = col_frag<T, VS>(vb + (u * 32 + kk * 16) * VS + d * 32, lane);
+                    if (__any(not_finite<T>(v))) {
+                        frag seen;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int key = u * 32 + kk * 16 + 8 * (j / 4) + j % 4;
+                            seen[j] = (T)(key >= see_lo && key < see_hi ? 1.0f : 0.0f);
+                        }
+                        frag up, down, nan;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float f = (float)v[j];
+                            up[j] = (T)(f > 3.402823466e38f ? 1.0f : 0.0f);
+                            down[j] = (T)(f < -3.402823466e38f ? 1.0f : 0.0f);
+                            nan[j] = (T)(f != f ? 1.0f : 0.0f);
+                            if (!(__builtin_fabsf(f) <= 3.402823466e38f)) v[j] = (T)0.0f;
+                        }
+                        f32x16 z;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+                        const f32x16 nu = mma(up, seen, z), nd = mma(down, seen, z), nn = mma(nan, seen, z);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            o[d][i] += (nu[i] > 0.0f ? __builtin_inff() : 0.0f) + (nd[i] > 0.0f ? -__builtin_inff() : 0.0f) +
+                                       (nn[i] > 0.0f ? __builtin_nanf("") : 0.0f);
+                    }
+                    o[d] = mma(v, b, o[d]);
+                }
+            }
+    };
+
+    T *buf = (T *)lds;
+    if (RW > 1) {
+        look_up(first);
+        fetch();
+        look_up(first + 1);
+        if (first < last) put(buf);
+        for (u32 i = first; i < last; ++i) {
+            __syncthreads();
+            if (i + 1 < last) {
+                fetch();
+                look_up(i + 2);
+            }
+            work(i, buf + (i - first & 1) * Shape::TILE);
+            // the other buffer was read before this round's barrier
+            if (i + 1 < last) put(buf + (i + 1 - first & 1) * Shape::TILE);
+        }
+    } else {
+        buf += kw * Shape::TILE;
+        look_up(first + kw);
+        fetch();
+        look_up(first + kw + KW);
+        for (u32 i = first + kw; i < last; i += KW) {
+            put(buf);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (i + KW < last) {
+                fetch();
+                look_up(i + 2 * KW);
+            }
+            work(i, buf);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    l += __shfl_xor(l, 32);
+
+    // Result of rows in this wave (or of the block's 32 rows): O^T holds entry 32 d + 8 (i / 4) + 4 half + i % 4 of its row.
+    const bool split_up = r.n_splits > 1;
+    if (KW == 1) {
+        if (row0 + (lane & 31) >= r.rows) return;
+        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        const float lse2 = l > 0.0f || l != l ? __builtin_fmaf(m, a.c, __log2f(l)) : -__builtin_inff();
+        const u64 at = (u64)(r.start + token) * a.heads + head;
+        if (half == 0) {
+            if (split_up)
+                a.part_lse[(u64)split * a.n_tokens * a.heads + at] = lse2;
+            else if (a.lse)
+                a.lse[at] = lse2 * 0.693147180559945309f;
+        }
+        float *part = a.part + ((u64)split * a.n_tokens * a.heads + at) * a.head_dim;
+        T *out = (T *)a.out + (i64)(r.start + token) * a.os[0] + head * a.os[1];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const u32 e = d * 32 + g * 8 + half * 4;
+                if (e >= a.head_dim) continue;
+                Pack<float, 4> x;
+                Pack<T, 4> y;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x.v[i] = l > 0.0f || l != l ? o[d][g * 4 + i] * inv : 0.0f;
+                    y.v[i] = (T)x.v[i];
+                }
+                if (split_up)
+                    store_pack<4>(part + e, x);
+                else
+                    store_pack<4>(out + e, y);
+            }
+        return;
+    }
+    // join the waves' results: [KW][32][DP] sums, then [KW][32] maxima and sums
+    float *jo = (float *)lds, *jm = jo + KW * 32 * DP, *jl = jm + KW * 32;
+    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            Pack<float, 4> x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.v[i] = o[d][g * 4 + i];
+            *(float4 *)(jo + (kw * 32 + (lane & 31)) * DP + d * 32 + g * 8 + half * 4) = make_float4(x.v[0], x.v[1], x.v[2], x.v[3]);
+        }
+    if (half == 0) {
+        jm[kw * 32 + lane] = m;
+        jl[kw * 32 + lane] = l;
+    }
+    __syncthreads();
+    const u32 n_rows = min(32u, r.rows - r.first_row), quads = a.head_dim / 4;
+    for (u32 x = threadIdx.x; x < n_rows * quads; x += 64 * KW) {
+        const u32 jr = x / quads, e = x % quads * 4;
+        float top = -__builtin_inff(), sum = 0.0f, f[KW];
+#pragma unroll
+        for (int w = 0; w < KW; ++w) top = fmaxf(top, jm[w * 32 + jr]);
+        float4 acc = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+            const float mw = jm[w * 32 + jr];
+            f[w] = mw == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((mw - top) * a.c);
+            const float lw = jl[w * 32 + jr];
+            // a wave that saw no key has nothing to add; one whose sum is NaN has
+            if (mw == -__builtin_inff() && lw == lw) continue;
+            if (lw != lw) f[w] = 1.0f;
+            sum = __builtin_fmaf(f[w], lw, sum);
+            const float4 y = *(const float4 *)(jo + (w * 32 + jr) * DP + e);
+            acc.x = __builtin_fmaf(f[w], y.x, acc.x);
+            acc.y = __builtin_fmaf(f[w], y.y, acc.y);
+            acc.z = __builtin_fmaf(f[w], y.z, acc.z);
+            acc.w = __builtin_fmaf(f[w], y.w, acc.w);
+        }
+        const bool some = sum > 0.0f || sum != sum;
+        const float inv = some ? 1.0f / sum : 0.0f;
+        const float lse2 = some ? __builtin_fmaf(top, a.c, __log2f(sum)) : -__builtin_inff();
+        const u32 jrow = r.first_row + jr, jt = r.start + jrow / a.group, jh = kv_head * a.group + jrow % a.group;
+        const u64 at = (u64)jt * a.heads + jh;
+        Pack<float, 4> res = {{some ? acc.x * inv : 0.0f, some ? acc.y * inv : 0.0f, some ? acc.z * inv : 0.0f, some ? acc.w * inv : 0.0f}};
+        if (split_up) {
+            if (e == 0) a.part_lse[(u64)split * a.n_tokens * a.heads + at] = lse2;
+            store_pack<4>(a.part + ((u64)split * a.n_tokens * a.heads + at) * a.head_dim + e, res);
+        } else {
+            if (e == 0 && a.lse) a.lse[at] = lse2 * 0.693147180559945309f;
+            Pack<T, 4> y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y.v[i] = (T)res.v[i];
+            store_pack<4>((T *)a.out + (i64)jt * a.os[0] + jh * a.os[1] + e, y);
+        }
+    }
+}
+
+// Joins the splits of a row: a wave per (token, head).
+template <class T, int ROWS, int TK>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+    const u64 at = (u64)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const u32 lane = threadIdx.x & 63, token = (u32)(at / a.heads), head = (u32)(at % a.heads);
+    if (token >= a.n_tokens) return;
+    RowTile r;
+    u32 lo = 0, hi = a.n_seq;
+    while (hi - lo > 1) {
+        const u32 mid = (lo + hi) >> 1;
+        if ((i64)a.q_start[mid] <= (i64)token)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    const int s = min(max(a.q_start[lo], 0), (int)a.n_tokens), e = max(min(a.q_start[lo + 1], (int)a.n_tokens), s);
+    if ((int)token < s || (int)token >= e) return;
+    r.seq = lo;
+    r.start = s;
+    r.n = e - s;
+    r.rows = r.n * a.group;
+    r.first_row = ((token - s) * a.group + head % a.group) / ROWS * ROWS;
+    key_range<ROWS, TK>(a, r);
+    if (r.n_splits <= 1) return;  // the row has been written
+    const u64 step = (u64)a.n_tokens * a.heads;
+    float top = -__builtin_inff();
+    for (u32 i = 0; i < r.n_splits; ++i) top = fmaxf(top, a.part_lse[i * step + at]);
+    float sum = 0.0f, acc[4] = {0, 0, 0, 0};
+    for (u32 i = 0; i < r.n_splits; ++i) {
+        const float z = a.part_lse[i * step + at];
+        if (z == -__builtin_inff()) continue;
+        const float f = z != z ? 1.0f : __builtin_amdgcn_exp2f(z - top);
+        sum += z != z ? z : f;
+        const float *p = a.part + (i * step + at) * a.head_dim;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k * 64 + lane < a.head_dim) acc[k] = __builtin_fmaf(f, p[k * 64 + lane], acc[k]);
+    }
+    const bool some = sum > 0.0f || sum != sum;
+    if (a.lse && lane == 0) a.lse[at] = some ? (top + __log2f(sum)) * 0.693147180559945309f : -__builtin_inff();
+    T *out = (T *)a.out + (i64)token * a.os[0] + head * a.os[1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (k * 64 + lane < a.head_dim) out[k * 64 + lane] = (T)(some ? acc[k] / sum : 0.0f);
+}
+
+// ---- host ----
+struct AttendPlan {
+    bool wide;          // four waves of 32 rows on shared tiles
+    u32 dp, tiles, splits, min_tiles;
+    u64 work_bytes;
+};
+
+// Which kernel and how many splits, from the sizes alone.
+static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
+    const ckks_clear_pages_t &g = p.pages;
+    const ckks_clear_batch_t &b = p.batch;
+    if (!clear_dtype_ok(g.dtype) || !g.head_dim || g.head_dim % 8 || g.head_dim > 256 || !g.kv_heads || !p.heads || p.heads % g.kv_heads ||
+        p.heads > 1u << 16)
+        return false;
+    const u64 group = p.heads / g.kv_heads, rows = (u64)b.n_tokens * group, seqs = std::min(b.n_seq, b.n_tokens);
+    const u64 keys = (u64)b.table_width * g.page_size;
+    if (rows >= 1u << 31 || keys >= 1u << 31 || b.n_seq >= 1u << 31) return false;
+    n.dp = g.head_dim <= 64 ? 64 : g.head_dim <= 128 ? 128 : 256;
+    const bool f32 = g.dtype == CKKS_CLEAR_F32;
+    // Sharing tiles reads keys and values a quarter as often; it needs enough row tiles of 128 to fill 256 CUs.
+    const u64 wide_blocks = (rows / 128) * g.kv_heads;
+    n.wide = wide_blocks >= 256 || (f32 && n.dp == 256);
+    const u64 r = n.wide ? 128 : 32;
+    const u64 tiles = rows / r + seqs;                       // at most
+    const u64 likely = seqs ? seqs * ((rows / seqs + r - 1) / r) : 0;
+    const u64 blocks = std::max<u64>(likely * g.kv_heads, 1);
+    const u32 tk = n.wide && !f32 && n.dp <= 128 ? 64 : 32;
+    // A split has 512 keys at least.  Eight blocks for each CU: sequences of different lengths then even out.
+    n.min_tiles = 512 / tk;
+    const u64 most = std::max<u64>(1, keys / 512);
+    n.splits = (u32)std::min<u64>(most, blocks >= 2048 ? 1 : (2048 + blocks - 1) / blocks);
+    if (tiles * g.kv_heads * n.splits >= 1u << 31) return false;
+    n.tiles = (u32)tiles;
+    n.work_bytes = n.splits > 1 ? (u64)n.splits * b.n_tokens * p.heads * (g.head_dim + 1) * 4 : 0;
+    return true;
+}
+
+template <class T, int DP, int RW, int KW, int TK, int OCC>
+static int launch_attend(const AttendArgs &a, hipStream_t st) {
+    hipLaunchKernelGGL((attend_kernel<T, DP, RW, KW, TK, OCC>), dim3(a.kv_heads * a.splits * a.tiles), dim3(64 * RW * KW), 0, st, a);
+    CKKS_LAUNCH_CHECK("attend_kernel");
+    if (a.splits > 1) {
+        hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK>), dim3((u32)(((u64)a.n_tokens * a.heads + 3) / 4)), dim3(256), 0, st, a);
+        CKKS_LAUNCH_CHECK("attend_join_kernel");
+    }
+    return CKKS_OK;
+}
+template <class T>
+static int launch_attend(const AttendArgs &a, const AttendPlan &n, hipStream_t st) {
+    constexpr bool f32 = sizeof(T) == 4;
+    if (n.wide) {
+        if (n.dp == 64) return launch_attend<T, 64, 4, 1, f32 ? 32 : 64, 2>(a, st);
+        if (n.dp == 128) return launch_attend<T, 128, 4, 1, f32 ? 32 : 64, f32 ? 1 : 2>(a, st);
+        return launch_attend<T, 256, 4, 1, 32, 1>(a, st);
+    }
+    if (n.dp == 64) return launch_attend<T, 64, 1, 4, 32, f32 ? 1 : 2>(a, st);
+    if (n.dp == 128) return launch_attend<T, 128, 1, 4, 32, f32 ? 1 : 2>(a, st);
+    if constexpr (!f32) return launch_attend<T, 256, 1, 4, 32, 1>(a, st);
+    return CKKS_E_INVAL;  // 32-bit rows of 256 always share tiles (plan_attend)
+}
+
+}  // namespace ckks
+
+using namespace ckks;
+
+extern "C" {
+
+uint64_t ckks_clear_attend_work_bytes(const ckks_clear_attend_t *p) {
+    AttendPlan n;
+    return p && plan_attend(*p, n) ? n.work_bytes : 0;
+}
+
+int ckks_clear_attend(const ckks_clear_attend_t *p, void *stream) {
+    const char *who = "ckks_clear_attend";
+    if (!p) {
+        set_error("%s: null argument", who);
+        return CKKS_E_INVAL;
+    }
+    const ckks_clear_pages_t &g = p->pages;
+    const ckks_clear_batch_t &b = p->batch;
+    if (int rc = check_cache(who, g, b)) return rc;
+    AttendPlan n;
+    if (!plan_attend(*p, n)) {
+        set_error("%s: %u heads over %u kv heads, %u tokens", who, p->heads, g.kv_heads, b.n_tokens);
+        return CKKS_E_INVAL;
+    }
+    if ((p->flags & ~CKKS_CLEAR_CAUSAL) || (p->window && !(p->flags & CKKS_CLEAR_CAUSAL)) || !(p->scale > 0.0f) || !std::isfinite(p->scale)) {
+        set_error("%s: flags %u, window %u (causal only), scale %g", who, p->flags, p->window, (double)p->scale);
+        return CKKS_E_INVAL;
+    }
+    if (!b.n_tokens || !b.n_seq) return CKKS_OK;
+    if (!p->d_q || !p->d_out) {
+        set_error("%s: null argument", who);
+        return CKKS_E_INVAL;
+    }
+    if (n.work_bytes > p->work_bytes || (n.work_bytes && (!p->d_work || (uintptr_t)p->d_work % 16))) {
+        set_error("%s: workspace of %llu bytes, needs %llu (16-byte aligned)", who, (unsigned long long)p->work_bytes, (unsigned long long)n.work_bytes);
+        return CKKS_E_INVAL;
+    }
+    const u32 e = clear_dtype_bytes(g.dtype);
+    const Extent out[3] = {extent(p->d_out, e, {{b.n_tokens, p->out_stride[0]}, {p->heads, p->out_stride[1]}, {g.head_dim, 1}}),
+                           extent(p->d_lse, 4, {{p->d_lse ? b.n_tokens : 0, p->heads}, {p->heads, 1}}), extent(p->d_work, 1, {{n.work_bytes, 1}})};
+    const Extent in[6] = {extent(p->d_q, e, {{b.n_tokens, p->q_stride[0]}, {p->heads, p->q_stride[1]}, {g.head_dim, 1}}),
+                          extent(g.d_k, e, {{g.n_pages, g.k_stride[0]}, {g.kv_heads, g.k_stride[1]}, {g.page_size, g.k_stride[2]}, {g.head_dim, 1}}),
+                          extent(g.d_v, e, {{g.n_pages, g.v_stride[0]}, {g.kv_heads, g.v_stride[1]}, {g.page_size, g.v_stride[2]}, {g.head_dim, 1}}),
+                          extent(b.d_q_start, 4, {{b.n_seq + 1, 1}}),
+                          extent(b.d_kv_len, 4, {{b.n_seq, 1}}),
+                          extent(b.d_page_table, 4, {{b.n_seq, b.table_stride}, {b.table_width, 1}})};
+    bool bad = overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2]);
+    for (const Extent &o : out)
+        for (const Extent &i : in) bad |= overlap(o, i);
+    if (bad) {
+        set_error("%s: an output overlaps another array", who);
+        return CKKS_E_INVAL;
+    }
+    AttendArgs a{};
+    a.q = p->d_q, a.k = g.d_k, a.v = g.d_v, a.out = p->d_out, a.lse = p->d_lse;
+    a.part_lse = (float *)p->d_work;
+    a.part = a.part_lse;
+    if (n.splits > 1) {  // partial results first: 16-byte rows where head_dim is a multiple of 4
+        a.part = (float *)p->d_work;
+        a.part_lse = a.part + (u64)n.splits * b.n_tokens * p->heads * g.head_dim;
+    }
+    for (int i = 0; i < 2; ++i) a.qs[i] = p->q_stride[i], a.os[i] = p->out_stride[i];
+    for (int i = 0; i < 3; ++i) a.ks[i] = g.k_stride[i], a.vs[i] = g.v_stride[i];
+    a.ts = b.table_stride, a.q_start = b.d_q_start, a.kv_len = b.d_kv_len, a.table = b.d_page_table;
+    a.n_seq = b.n_seq, a.n_tokens = b.n_tokens, a.n_pages = g.n_pages, a.page_size = g.page_size, a.table_width = b.table_width;
+    a.kv_heads = g.kv_heads, a.heads = p->heads, a.group = p->heads / g.kv_heads, a.head_dim = g.head_dim;
+    a.window = p->window, a.causal = p->flags & CKKS_CLEAR_CAUSAL;
+    a.page_shift = (g.page_size & (g.page_size - 1)) ? -1 : 31 - __builtin_clz(g.page_size);
+    a.tiles = n.tiles, a.splits = n.splits, a.min_tiles = n.min_tiles;
+    a.c = p->scale * 1.44269504088896340736f;
+    hipStream_t st = (hipStream_t)stream;
+    return g.dtype == CKKS_CLEAR_F32   ? launch_attend<float>(a, n, st)
+           : g.dtype == CKKS_CLEAR_F16 ? launch_attend<f16>(a, n, st)
+                                       : launch_attend<bf16>(a, n, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,96 @@
+// Types, wide loads and wave reductions of the steps in the clear (clear_*.hip).
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "../../include/ckks_clear.h"
+#include "ckks_internal.h"
+
+namespace ckks {
+
+typedef int64_t i64;
+typedef _Float16 f16;
+typedef __bf16 bf16;
+
+// N values in one access.  A row of an odd width starts wherever its type allows; global memory takes such an address at
+// full width, so there is no second code path for it.
+template <class T, int N>
+struct Pack {
+    T v[N];
+};
+template <int N, class T>
+__device__ __forceinline__ Pack<T, N> load_pack(const T *p) {
+    Pack<T, N> r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    return r;
+}
+template <int N, class T>
+__device__ __forceinline__ void store_pack(T *p, const Pack<T, N> &x) {
+    __builtin_memcpy(p, &x, sizeof(x));
+}
+// The first `n` of N values, zeros behind them.
+template <int N, class T>
+__device__ __forceinline__ Pack<T, N> load_part(const T *p, int n) {
+    if (n >= N) return load_pack<N>(p);
+    Pack<T, N> r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.v[i] = i < n ? p[i] : (T)0.0f;
+    return r;
+}
+template <int N, class T>
+__device__ __forceinline__ void store_part(T *p, const Pack<T, N> &x, int n) {
+    if (n >= N) {
+        store_pack<N>(p, x);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = x.v[i];
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+    return x;
+}
+
+// ---- host ----
+inline bool clear_dtype_ok(u32 d) { return d <= CKKS_CLEAR_BF16; }
+inline u32 clear_dtype_bytes(u32 d) { return d == CKKS_CLEAR_F32 ? 4 : 2; }
+
+// Bytes [lo, hi) that an array of rows touches: `n` counts and strides (in elements), outermost first.
+struct Extent {
+    uintptr_t lo, hi;
+};
+inline Extent extent(const void *p, u32 elem_bytes, std::initializer_list<std::pair<u64, i64>> dims) {
+    i64 lo = 0, hi = 0;
+    for (const auto &d : dims) {
+        if (!d.first) return {0, 0};
+        const i64 span = (i64)(d.first - 1) * d.second;
+        (span < 0 ? lo : hi) += span;
+    }
+    return {(uintptr_t)p + (uintptr_t)(lo * elem_bytes), (uintptr_t)p + (uintptr_t)((hi + 1) * elem_bytes)};
+}
+// What append and attend ask of the pages and the batch alike.
+inline int check_cache(const char *who, const ckks_clear_pages_t &g, const ckks_clear_batch_t &b) {
+    if (!clear_dtype_ok(g.dtype) || !g.head_dim || g.head_dim % 8 || g.head_dim > 256 || !g.kv_heads || g.kv_heads > 1u << 16 || !g.page_size) {
+        set_error("%s: pages of type %u, %u rows, %u heads of %u entries", who, g.dtype, g.page_size, g.kv_heads, g.head_dim);
+        return CKKS_E_INVAL;
+    }
+    if (b.n_tokens >= 1u << 31 || b.n_seq >= 1u << 31 || (u64)b.table_width * g.page_size >= 1u << 31) {
+        set_error("%s: %u tokens, %u sequences of up to %u pages of %u", who, b.n_tokens, b.n_seq, b.table_width, g.page_size);
+        return CKKS_E_INVAL;
+    }
+    if (b.n_tokens && !b.n_seq) {
+        set_error("%s: %u tokens of no sequence", who, b.n_tokens);
+        return CKKS_E_INVAL;
+    }
+    if (b.n_tokens && (!b.d_q_start || !b.d_kv_len || (b.table_width && !b.d_page_table) || (g.n_pages && (!g.d_k || !g.d_v)))) {
+        set_error("%s: null argument", who);
+        return CKKS_E_INVAL;
+    }
+    return CKKS_OK;
+}
+
+inline bool overlap(const Extent &a, const Extent &b) { return a.lo < b.hi && b.lo < a.hi && a.lo != a.hi && b.lo != b.hi; }
+
+}  // namespace ckks

@@ -1,0 +1,470 @@
+// Layer norm and its gradient.  A group of threads holds a row in registers, so every array is read once: both calls are
+// bound by memory.  The weight's and bias's gradients are column sums: each group keeps them for the columns that it holds
+// over all its rows, writes them once, and a second kernel adds the groups' sums in their order.
+#include <algorithm>
+
+#include "clear_device.h"
+
+namespace ckks {
+
+struct NormArgs {
+    const void *x, *dy, *w, *b;
+    void *y;                    // forward: y, gradient: dx
+    float *mean, *rstd;
+    float *part;                // gradient: [blocks][2][cols] sums of dy*xh and dy, or null
+    i64 xs, dys, ys;
+    u32 rows, cols;
+    float eps;
+};
+
+// Sums of two values over the TPR threads of a group.  `slot` alternates between two halves of the exchange area, so one
+// barrier per call is enough: a wave can be at most one call ahead.
+template <int TPR>
+__device__ __forceinline__ void group_sum2(float &p, float &q, float (*ex)[2][2], u32 &slot) {
+    p = wave_sum(p);
+    q = wave_sum(q);
+    if (TPR > 64) {
+        const u32 wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            ex[wave][slot][0] = p;
+            ex[wave][slot][1] = q;
+        }
+        __syncthreads();
+        p = q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TPR / 64; ++i) {
+            p += ex[i][slot][0];
+            q += ex[i][slot][1];
+        }
+        slot ^= 1;
+    }
+}
+
+// E entries of a row per thread, in chunks of 16 bytes that lie TPR chunks apart.
+template <class T, class TW, int TPR, int E>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
+    constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
+    __shared__ float ex[TPR / 64][2][2];
+    u32 slot = 0;
+    const u32 t = threadIdx.x % TPR, groups = gridDim.x * (THREADS / TPR);
+    int n[K];
+    float w[K][V], b[K][V];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const u32 col = (k * TPR + t) * V;
+        n[k] = col < a.cols ? (int)min(a.cols - col, (u32)V) : 0;
+        const Pack<TW, V> pw = a.w ? load_part<V>((const TW *)a.w + col, n[k]) : Pack<TW, V>{};
+        const Pack<TW, V> pb = a.b ? load_part<V>((const TW *)a.b + col, n[k]) : Pack<TW, V>{};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[k][i] = a.w ? (float)pw.v[i] : 1.0f;
+            b[k][i] = (float)pb.v[i];
+        }
+    }
+    const float inv = 1.0f / (float)a.cols;
+    for (u32 row = blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR; row < a.rows; row += groups) {
+        const T *x = (const T *)a.x + (i64)row * a.xs;
+        T *y = (T *)a.y + (i64)row * a.ys;
+        float v[K][V], s = 0.0f, none = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const Pack<T, V> p = load_part<V>(x + (k * TPR + t) * V, n[k]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                v[k][i] = (float)p.v[i];
+                s += v[k][i];
+            }
+        }
+        group_sum2<TPR>(s, none, ex, slot);
+        const float mean = s * inv;
+        float q = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = i < n[k] ? v[k][i] - mean : 0.0f;
+                v[k][i] = d;
+                q = __builtin_fmaf(d, d, q);
+            }
+        none = 0.0f;
+        group_sum2<TPR>(q, none, ex, slot);
+        const float r = 1.0f / sqrtf(__builtin_fmaf(q, inv, a.eps));
+        if (t == 0 && a.mean) {
+            a.mean[row] = mean;
+            a.rstd[row] = r;
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            Pack<T, V> p;
+#pragma unroll
+            for (int i = 0; i < V; ++i) p.v[i] = (T)__builtin_fmaf(v[k][i] * r, w[k][i], b[k][i]);
+            store_part<V>(y + (k * TPR + t) * V, p, n[k]);
+        }
+    }
+}
+
+template <class T, class TW, int TPR, int E>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormArgs a) {
+    constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR, GROUPS = THREADS / TPR;
+    __shared__ float ex[TPR / 64][2][2];
+    u32 slot = 0;
+    const u32 t = threadIdx.x % TPR, groups = gridDim.x * GROUPS;
+    int n[K];
+    float w[K][V], dw[K][V], db[K][V];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const u32 col = (k * TPR + t) * V;
+        n[k] = col < a.cols ? (int)min(a.cols - col, (u32)V) : 0;
+        const Pack<TW, V> pw = a.w ? load_part<V>((const TW *)a.w + col, n[k]) : Pack<TW, V>{};
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            w[k][i] = a.w ? (float)pw.v[i] : 1.0f;
+            dw[k][i] = db[k][i] = 0.0f;
+        }
+    }
+    const float inv = 1.0f / (float)a.cols;
+    for (u32 row = blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += groups) {
+        const T *x = (const T *)a.x + (i64)row * a.xs, *dy = (const T *)a.dy + (i64)row * a.dys;
+        const float mean = a.mean[row], r = a.rstd[row];
+        float xh[K][V], g[K][V], s1 = 0.0f, s2 = 0.0f;
+        Pack<T, V> px[K], pd[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            px[k] = load_part<V>(x + (k * TPR + t) * V, n[k]);
+            pd[k] = load_part<V>(dy + (k * TPR + t) * V, n[k]);
+        }
+        // behind the row's end dy is 0, and so is everything that it meets
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float d = (float)pd[k].v[i], h = ((float)px[k].v[i] - mean) * r;
+                xh[k][i] = h;
+                g[k][i] = d * w[k][i];
+                dw[k][i] = __builtin_fmaf(d, h, dw[k][i]);
+                db[k][i] += d;
+                s1 += g[k][i];
+                s2 = __builtin_fmaf(g[k][i], h, s2);
+            }
+        if (!a.y) continue;
+        group_sum2<TPR>(s1, s2, ex, slot);
+        s1 *= inv;
+        s2 *= inv;
+        T *dx = (T *)a.y + (i64)row * a.ys;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            Pack<T, V> p;
+#pragma unroll
+            for (int i = 0; i < V; ++i) p.v[i] = (T)(r * (g[k][i] - s1 - xh[k][i] * s2));
+            store_part<V>(dx + (k * TPR + t) * V, p, n[k]);
+        }
+    }
+    if (!a.part) return;
+    float *part = a.part + (size_t)blockIdx.x * 2 * a.cols;
+    if (GROUPS == 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const u32 col = (k * TPR + t) * V + i;
+                if (i < n[k]) {
+                    part[col] = dw[k][i];
+                    part[a.cols + col] = db[k][i];
+                }
+            }
+        return;
+    }
+    // the block's groups hold the same columns: joined here, a quarter as many sums reach memory
+    __shared__ float join[GROUPS][2][TPR * V];
+    const u32 gr = threadIdx.x / TPR;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            join[gr][0][t * V + i] = dw[k][i];
+            join[gr][1][t * V + i] = db[k][i];
+        }
+        __syncthreads();
+        for (u32 c = threadIdx.x; c < 2 * TPR * V; c += THREADS) {
+            const u32 which = c / (TPR * V), col = c % (TPR * V);
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) s += join[i][which][col];
+            if ((u32)k * TPR * V + col < a.cols) part[which * (size_t)a.cols + k * TPR * V + col] = s;
+        }
+    }
+}
+
+// Rows wider than the registers of a block: the same sums in loops over the row, which comes from the caches again.
+template <class T, class TW>
+__global__ __launch_bounds__(1024) void norm_wide_kernel(NormArgs a) {
+    __shared__ float ex[16][2][2];
+    u32 slot = 0;
+    const float inv = 1.0f / (float)a.cols;
+    for (u32 row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = (const T *)a.x + (i64)row * a.xs;
+        T *y = (T *)a.y + (i64)row * a.ys;
+        float s = 0.0f, q = 0.0f, none = 0.0f;
+        for (u64 c = threadIdx.x; c < a.cols; c += 1024) s += (float)x[c];
+        group_sum2<1024>(s, none, ex, slot);
+        const float mean = s * inv;
+        for (u64 c = threadIdx.x; c < a.cols; c += 1024) {
+            const float d = (float)x[c] - mean;
+            q = __builtin_fmaf(d, d, q);
+        }
+        none = 0.0f;
+        group_sum2<1024>(q, none, ex, slot);
+        const float r = 1.0f / sqrtf(__builtin_fmaf(q, inv, a.eps));
+        if (threadIdx.x == 0 && a.mean) {
+            a.mean[row] = mean;
+            a.rstd[row] = r;
+        }
+        for (u64 c = threadIdx.x; c < a.cols; c += 1024) {
+            const float w = a.w ? (float)((const TW *)a.w)[c] : 1.0f, b = a.b ? (float)((const TW *)a.b)[c] : 0.0f;
+            y[c] = (T)__builtin_fmaf(((float)x[c] - mean) * r, w, b);
+        }
+    }
+}
+
+// Column sums first (dx may take the place of dy), then dx.
+template <class T>
+__global__ __launch_bounds__(256) void norm_grad_wide_cols_kernel(NormArgs a, u32 parts) {
+    const u64 c = (u64)blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.cols) return;
+    float dw = 0.0f, db = 0.0f;
+    for (u32 row = blockIdx.y; row < a.rows; row += parts) {
+        const float d = (float)((const T *)a.dy)[(i64)row * a.dys + c];
+        dw = __builtin_fmaf(d, ((float)((const T *)a.x)[(i64)row * a.xs + c] - a.mean[row]) * a.rstd[row], dw);
+        db += d;
+    }
+    float *part = a.part + (size_t)blockIdx.y * 2 * a.cols;
+    part[c] = dw;
+    part[a.cols + c] = db;
+}
+template <class T, class TW>
+__global__ __launch_bounds__(1024) void norm_grad_wide_kernel(NormArgs a) {
+    __shared__ float ex[16][2][2];
+    u32 slot = 0;
+    const float inv = 1.0f / (float)a.cols;
+    for (u32 row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = (const T *)a.x + (i64)row * a.xs, *dy = (const T *)a.dy + (i64)row * a.dys;
+        T *dx = (T *)a.y + (i64)row * a.ys;
+        const float mean = a.mean[row], r = a.rstd[row];
+        float s1 = 0.0f, s2 = 0.0f;
+        for (u64 c = threadIdx.x; c < a.cols; c += 1024) {
+            const float g = (float)dy[c] * (a.w ? (float)((const TW *)a.w)[c] : 1.0f);
+            s1 += g;
+            s2 = __builtin_fmaf(g, ((float)x[c] - mean) * r, s2);
+        }
+        group_sum2<1024>(s1, s2, ex, slot);
+        s1 *= inv;
+        s2 *= inv;
+        for (u64 c = threadIdx.x; c < a.cols; c += 1024) {
+            const float g = (float)dy[c] * (a.w ? (float)((const TW *)a.w)[c] : 1.0f);
+            dx[c] = (T)(r * (g - s1 - ((float)x[c] - mean) * r * s2));
+        }
+    }
+}
+
+// dw[c], db[c] = the parts' sums in order: 64 columns per block, 16 threads share a column's parts.
+template <class TW>
+__global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restrict__ part, u32 parts, u32 cols, TW *dw, TW *db) {
+    __shared__ float join[16][64];
+    const u32 c = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const u64 col = (u64)blockIdx.x * 64 + c;
+    TW *out = blockIdx.y ? db : dw;
+    if (!out) return;
+    float s = 0.0f;
+    if (col < cols)
+#pragma unroll 4
+        for (u32 p = q; p < parts; p += 16) s += part[((size_t)p * 2 + blockIdx.y) * cols + col];
+    join[q][c] = s;
+    __syncthreads();
+    if (q == 0 && col < cols) {
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += join[i][c];
+        out[col] = (TW)s;
+    }
+}
+
+// Threads per row and entries per thread: the smallest group whose registers hold the row at up to 32 entries a thread
+// (16 where 1024 threads share the register file).  0: none does.
+struct NormShape {
+    u32 tpr, e;
+};
+static NormShape norm_shape(u32 cols) {
+    if (cols <= 64 * 32) return {64, cols <= 64 * 8 ? 8u : cols <= 64 * 16 ? 16u : 32u};
+    if (cols <= 256 * 32) return {256, cols <= 256 * 16 ? 16u : 32u};
+    if (cols <= 1024 * 16) return {1024, 16};
+    return {0, 0};
+}
+// Blocks of the gradient, each of which leaves one pair of column sums: two to four blocks for each of 256 CUs.
+static u32 norm_grad_blocks(u32 rows, u32 cols) {
+    const NormShape s = norm_shape(cols);
+    if (!s.tpr) return std::min<u32>(rows, 64);
+    const u32 per = s.tpr == 64 ? 4 : 1;
+    return std::min<u32>((rows + per - 1) / per, 512);
+}
+
+template <class T, class TW>
+static void launch_norm(const NormArgs &a, hipStream_t st) {
+    const NormShape s = norm_shape(a.cols);
+    const u32 per = s.tpr == 64 ? 4 : 1;
+    const u32 blocks = std::min<u32>((a.rows + per - 1) / per, 2048);
+#define CKKS_NORM(TPR, E) \
+    if (s.tpr == TPR && s.e == E) {                                                                                      \
+        hipLaunchKernelGGL((norm_kernel<T, TW, TPR, E>), dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);         \
+        return;                                                                                                           \
+    }
+    CKKS_NORM(64, 8)
+    CKKS_NORM(64, 16)
+    CKKS_NORM(64, 32)
+    CKKS_NORM(256, 16)
+    CKKS_NORM(256, 32)
+    CKKS_NORM(1024, 16)
+#undef CKKS_NORM
+    hipLaunchKernelGGL((norm_wide_kernel<T, TW>), dim3(std::min<u32>(a.rows, 1024)), dim3(1024), 0, st, a);
+}
+
+template <class T, class TW>
+static void launch_norm_grad(const NormArgs &a, u32 blocks, hipStream_t st) {
+    const NormShape s = norm_shape(a.cols);
+#define CKKS_NORM(TPR, E) \
+    if (s.tpr == TPR && s.e == E) {                                                                                      \
+        hipLaunchKernelGGL((norm_grad_kernel<T, TW, TPR, E>), dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);    \
+        return;                                                                                                           \
+    }
+    CKKS_NORM(64, 8)
+    CKKS_NORM(64, 16)
+    CKKS_NORM(64, 32)
+    CKKS_NORM(256, 16)
+    CKKS_NORM(256, 32)
+    CKKS_NORM(1024, 16)
+#undef CKKS_NORM
+    if (a.part)
+        hipLaunchKernelGGL((norm_grad_wide_cols_kernel<T>), dim3((u32)(((u64)a.cols + 255) / 256), blocks), dim3(256), 0, st, a, blocks);
+    if (a.y)
+        hipLaunchKernelGGL((norm_grad_wide_kernel<T, TW>), dim3(std::min<u32>(a.rows, 1024)), dim3(1024), 0, st, a);
+}
+
+}  // namespace ckks
+
+using namespace ckks;
+
+// (T, TW) of a pair of types that the calls take
+#define CKKS_NORM_TYPES(F, ...)                                                     \
+    (dtype == CKKS_CLEAR_F32   ? F<float, float>(__VA_ARGS__)                       \
+     : dtype == CKKS_CLEAR_F16 ? (wtype == CKKS_CLEAR_F32 ? F<f16, float>(__VA_ARGS__) : F<f16, f16>(__VA_ARGS__)) \
+                               : (wtype == CKKS_CLEAR_F32 ? F<bf16, float>(__VA_ARGS__) : F<bf16, bf16>(__VA_ARGS__)))
+
+static int check_norm(const char *who, u32 rows, u32 cols, u32 dtype, u32 wtype) {
+    if (!clear_dtype_ok(dtype) || (wtype != CKKS_CLEAR_F32 && wtype != dtype)) {
+        set_error("%s: types %u and %u (weight): the weight has the rows' type or f32", who, dtype, wtype);
+        return CKKS_E_INVAL;
+    }
+    if (!cols || rows >= 1u << 31 || cols >= 1u << 31) {
+        set_error("%s: %u rows of %u entries", who, rows, cols);
+        return CKKS_E_INVAL;
+    }
+    return CKKS_OK;
+}
+
+extern "C" {
+
+int ckks_clear_layer_norm(const ckks_clear_norm_t *p, void *stream) {
+    if (!p || (p->rows && (!p->d_x || !p->d_y))) {
+        set_error("ckks_clear_layer_norm: null argument");
+        return CKKS_E_INVAL;
+    }
+    if (int rc = check_norm("ckks_clear_layer_norm", p->rows, p->cols, p->dtype, p->weight_dtype)) return rc;
+    if (!(p->eps >= 0.0f) || !p->d_mean != !p->d_rstd) {
+        set_error("ckks_clear_layer_norm: eps %g, or only one of d_mean and d_rstd", (double)p->eps);
+        return CKKS_E_INVAL;
+    }
+    if (!p->rows) return CKKS_OK;
+    const u32 dtype = p->dtype, wtype = p->weight_dtype, e = clear_dtype_bytes(dtype), we = clear_dtype_bytes(wtype);
+    const Extent x = extent(p->d_x, e, {{p->rows, p->x_stride}, {p->cols, 1}}), y = extent(p->d_y, e, {{p->rows, p->y_stride}, {p->cols, 1}});
+    const Extent w = extent(p->d_weight, we, {{p->d_weight ? p->cols : 0, 1}}), b = extent(p->d_bias, we, {{p->d_bias ? p->cols : 0, 1}});
+    const Extent m = extent(p->d_mean, 4, {{p->d_mean ? p->rows : 0, 1}}), r = extent(p->d_rstd, 4, {{p->d_rstd ? p->rows : 0, 1}});
+    const bool in_place = p->d_x == p->d_y && (p->x_stride == p->y_stride || p->rows == 1);
+    if ((!in_place && overlap(x, y)) || overlap(y, w) || overlap(y, b) || overlap(y, m) || overlap(y, r) || overlap(m, x) ||
+        overlap(r, x) || overlap(m, r) || overlap(m, w) || overlap(m, b) || overlap(r, w) || overlap(r, b)) {
+        set_error("ckks_clear_layer_norm: an output overlaps another array");
+        return CKKS_E_INVAL;
+    }
+    if (p->rows > 1 && (p->y_stride < 0 ? -p->y_stride : p->y_stride) < (i64)p->cols) {
+        set_error("ckks_clear_layer_norm: output rows overlap (stride %lld)", (long long)p->y_stride);
+        return CKKS_E_INVAL;
+    }
+    NormArgs a{};
+    a.x = p->d_x, a.w = p->d_weight, a.b = p->d_bias, a.y = p->d_y, a.mean = p->d_mean, a.rstd = p->d_rstd;
+    a.xs = p->x_stride, a.ys = p->y_stride, a.rows = p->rows, a.cols = p->cols, a.eps = p->eps;
+    CKKS_NORM_TYPES(launch_norm, a, (hipStream_t)stream);
+    CKKS_LAUNCH_CHECK("norm_kernel");
+    return CKKS_OK;
+}
+
+uint64_t ckks_clear_layer_norm_grad_work_bytes(uint32_t rows, uint32_t cols, uint32_t) {
+    return (u64)norm_grad_blocks(rows, cols) * 2 * cols * sizeof(float);
+}
+
+int ckks_clear_layer_norm_grad(const ckks_clear_norm_grad_t *p, void *stream) {
+    if (!p || (p->rows && (!p->d_x || !p->d_dy || !p->d_mean || !p->d_rstd))) {
+        set_error("ckks_clear_layer_norm_grad: null argument");
+        return CKKS_E_INVAL;
+    }
+    if (int rc = check_norm("ckks_clear_layer_norm_grad", p->rows, p->cols, p->dtype, p->weight_dtype)) return rc;
+    const u32 dtype = p->dtype, wtype = p->weight_dtype, e = clear_dtype_bytes(dtype), we = clear_dtype_bytes(wtype);
+    const bool params = p->d_dweight || p->d_dbias;
+    const u64 need = params ? ckks_clear_layer_norm_grad_work_bytes(p->rows, p->cols, dtype) : 0;
+    if (need > p->work_bytes || (need && (!p->d_work || (uintptr_t)p->d_work % 4))) {
+        set_error("ckks_clear_layer_norm_grad: workspace of %llu bytes, needs %llu (4-byte aligned)", (unsigned long long)p->work_bytes,
+                  (unsigned long long)need);
+        return CKKS_E_INVAL;
+    }
+    const Extent in[5] = {extent(p->d_x, e, {{p->rows, p->x_stride}, {p->cols, 1}}), extent(p->d_weight, we, {{p->d_weight ? p->cols : 0, 1}}),
+                          extent(p->d_mean, 4, {{p->rows, 1}}), extent(p->d_rstd, 4, {{p->rows, 1}}),
+                          extent(p->d_dy, e, {{p->rows, p->dy_stride}, {p->cols, 1}})};
+    const Extent out[4] = {extent(p->d_dx, e, {{p->d_dx ? p->rows : 0, p->dx_stride}, {p->cols, 1}}),
+                           extent(p->d_dweight, we, {{p->d_dweight ? p->cols : 0, 1}}), extent(p->d_dbias, we, {{p->d_dbias ? p->cols : 0, 1}}),
+                           extent(p->d_work, 1, {{need, 1}})};
+    const bool in_place = p->d_dx == p->d_dy && (p->dx_stride == p->dy_stride || p->rows == 1);
+    bool bad = false;
+    for (int o = 0; o < 4; ++o) {
+        for (int i = 0; i < 5; ++i) bad |= !(o == 0 && i == 4 && in_place) && overlap(out[o], in[i]);
+        for (int i = 0; i < o; ++i) bad |= overlap(out[o], out[i]);
+    }
+    if (bad) {
+        set_error("ckks_clear_layer_norm_grad: an output overlaps another array");
+        return CKKS_E_INVAL;
+    }
+    if (p->d_dx && p->rows > 1 && (p->dx_stride < 0 ? -p->dx_stride : p->dx_stride) < (i64)p->cols) {
+        set_error("ckks_clear_layer_norm_grad: output rows overlap (stride %lld)", (long long)p->dx_stride);
+        return CKKS_E_INVAL;
+    }
+    NormArgs a{};
+    a.x = p->d_x, a.dy = p->d_dy, a.w = p->d_weight, a.y = p->d_dx;
+    a.mean = (float *)p->d_mean, a.rstd = (float *)p->d_rstd, a.part = params ? (float *)p->d_work : nullptr;
+    a.xs = p->x_stride, a.dys = p->dy_stride, a.ys = p->dx_stride, a.rows = p->rows, a.cols = p->cols;
+    const u32 blocks = norm_grad_blocks(p->rows, p->cols);
+    hipStream_t st = (hipStream_t)stream;
+    if (p->rows && (a.y || params)) {
+        CKKS_NORM_TYPES(launch_norm_grad, a, blocks, st);
+        CKKS_LAUNCH_CHECK("norm_grad_kernel");
+    }
+    if (params) {
+        const dim3 grid((p->cols + 63) / 64, 2);
+        if (wtype == CKKS_CLEAR_F32)
+            hipLaunchKernelGGL(norm_parts_kernel<float>, grid, dim3(1024), 0, st, a.part, blocks, p->cols, (float *)p->d_dweight, (float *)p->d_dbias);
+        else if (wtype == CKKS_CLEAR_F16)
+            hipLaunchKernelGGL(norm_parts_kernel<f16>, grid, dim3(1024), 0, st, a.part, blocks, p->cols, (f16 *)p->d_dweight, (f16 *)p->d_dbias);
+        else
+            hipLaunchKernelGGL(norm_parts_kernel<bf16>, grid, dim3(1024), 0, st, a.part, blocks, p->cols, (bf16 *)p->d_dweight, (bf16 *)p->d_dbias);
+        CKKS_LAUNCH_CHECK("norm_parts_kernel");
+    }
+    return CKKS_OK;
+}
+
+}  // extern "C"

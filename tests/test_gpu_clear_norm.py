@@ -1,0 +1,182 @@
+"""Layer norm and its gradient against 64 bits, at the widths where the kernels change shape, and against differences."""
+import pytest
+import torch
+
+from tests.clear_util import TINY, TYPES, U, close, gen, norm_ref, randn
+
+pytestmark = pytest.mark.gpu
+
+# both sides of every line between group sizes, widths that are no multiple of an access, one entry, wider than a block
+WIDTHS = [1, 7, 64, 511, 513, 768, 1025, 2048, 2049, 4097, 8192, 8200, 16384, 16385, 20000]
+
+
+def inputs(rows, cols, dtype, seed, wtype=torch.float32):
+    g = gen(seed)
+    x = randn(g, rows, cols) * (0.25 + 3 * torch.rand(rows, 1, generator=g, device="cuda")) + randn(g, rows, 1)
+    w, b = (1 + 0.2 * randn(g, cols)).to(wtype), (0.2 * randn(g, cols)).to(wtype)
+    return x.to(dtype), w, b, randn(g, rows, cols, dtype=dtype)
+
+
+def ratio(x, rstd):
+    """How much larger than a row's deviation its values are: what cancels in x - mean."""
+    return 1 + x.double().abs().amax(-1, keepdim=True) * rstd
+
+
+def check(K, x, w, b, dy, eps=1e-5):
+    dtype = x.dtype
+    u = U[dtype]
+    y, mean, rstd = K.ckks_clear_layer_norm(x, w, b, eps)
+    want, m64, r64, xh = norm_ref(x, w, b, eps)
+    rho = ratio(x, r64)
+    wd = 1.0 if w is None else w.double().abs()
+    # sums of up to 32 entries one after the other, then a tree: 2^-18 is 64 roundings of 32 bits
+    close(mean.unsqueeze(-1), m64, 2.0**-18 * x.double().abs().amax(-1, keepdim=True) + 1e-30, "mean")
+    close(rstd.unsqueeze(-1), r64, 2.0**-18 * r64 * rho, "rstd")
+    bd = 0.0 if b is None else b.double().abs()
+    close(y, want, u * want.abs() + 2.0**-18 * (wd * (1 + xh.abs()) * rho + bd) + TINY[dtype], "y")
+    dx, dw, db = K.ckks_clear_layer_norm_grad(dy, x, mean, rstd, w)
+    d = dy.double()
+    g = d * (1.0 if w is None else w.double())
+    want = r64 * (g - g.mean(-1, keepdim=True) - xh * (g * xh).mean(-1, keepdim=True))
+    size = r64 * rho * (g.abs() + g.abs().mean(-1, keepdim=True) + xh.abs() * (g * xh).abs().mean(-1, keepdim=True))
+    close(dx, want, u * want.abs() + 2.0**-18 * size + TINY[dtype], "dx")
+    uw = U[dw.dtype]
+    deep = 2.0**-24 * (64 + x.shape[0] / 512 + 32)
+    close(dw, (d * xh).sum(0), uw * (d * xh).sum(0).abs() + (deep + 2.0**-18) * (d.abs() * (1 + xh.abs()) * rho).sum(0) + TINY[dw.dtype], "dw")
+    close(db, d.sum(0), uw * d.sum(0).abs() + (deep + 2.0**-18) * d.abs().sum(0) + TINY[dw.dtype], "db")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", WIDTHS)
+def test_against_64_bits(cols, dtype):
+    from paper_2604_09975_amd import clear as K
+    for rows in (1, 5) if cols > 4096 else (1, 3, 130):
+        check(K, *inputs(rows, cols, TYPES[dtype], cols + rows))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_and_parameters_of_the_rows_type(dtype):
+    from paper_2604_09975_amd import clear as K
+    t = TYPES[dtype]
+    check(K, *inputs(3001, 200, t, 1, t))
+    x, w, b, dy = inputs(700, 3000, t, 2, t)
+    check(K, x, w, b, dy)
+    check(K, x, None, None, dy)
+    check(K, x, w, None, dy, eps=0.5)
+
+
+def test_strides_places_and_shapes():
+    from paper_2604_09975_amd import clear as K
+    x, w, b, dy = inputs(60, 333, torch.bfloat16, 3)
+    want, mean, rstd = K.ckks_clear_layer_norm(x, w, b)
+    grads = K.ckks_clear_layer_norm_grad(dy, x, mean, rstd, w)
+    # columns of a wider array, at an odd offset
+    wide = torch.zeros(60, 1001, dtype=torch.bfloat16, device="cuda")
+    xs, ys = wide[:, 1:334], wide[:, 501:834]
+    xs.copy_(x)
+    with pytest.raises(Exception) as e:
+        K.ckks_clear_layer_norm(xs, w, b, out=ys)   # the extents of interleaved columns meet
+    assert "overlaps" in str(e.value)
+    wide2 = torch.zeros(60, 1001, dtype=torch.bfloat16, device="cuda")
+    ys = wide2[:, 501:834]
+    y, m2, r2 = K.ckks_clear_layer_norm(xs, w, b, out=ys)
+    assert torch.equal(ys, want) and torch.equal(m2, mean) and torch.equal(r2, rstd)
+    assert not wide2[:, :501].any() and not wide2[:, 834:].any()
+    ds = torch.zeros(60, 700, dtype=torch.bfloat16, device="cuda")[:, 3:336]
+    ds.copy_(dy)
+    got = K.ckks_clear_layer_norm_grad(ds, xs, mean, rstd, w, dx=ds)   # in place of dy
+    assert got[0] is ds and all(torch.equal(a, c) for a, c in zip(got, grads))
+    z = x.clone()
+    assert K.ckks_clear_layer_norm(z, w, b, out=z)[0] is z and torch.equal(z, want)
+    y3, m3, _ = K.ckks_clear_layer_norm(x.view(4, 15, 333), w, b)
+    assert y3.shape == (4, 15, 333) and m3.shape == (4, 15) and torch.equal(y3.view(60, 333), want)
+    y4, m4, r4 = K.ckks_clear_layer_norm(x, w, b, stats=False)
+    assert m4 is None and r4 is None and torch.equal(y4, want)
+    only = K.ckks_clear_layer_norm_grad(dy, x, mean, rstd, w, params=False)
+    assert torch.equal(only[0], grads[0]) and only[1] is None and only[2] is None
+    # one gradient row for all rows
+    row = dy[:1].expand(60, 333)
+    a, c = K.ckks_clear_layer_norm_grad(row, x, mean, rstd, w), K.ckks_clear_layer_norm_grad(row.contiguous(), x, mean, rstd, w)
+    assert all(torch.equal(p, q) for p, q in zip(a, c))
+    y, m, r = K.ckks_clear_layer_norm(x[:0], w, b)
+    assert y.shape == (0, 333)
+    dx, dw, db = K.ckks_clear_layer_norm_grad(dy[:0], x[:0], m, r, w)
+    assert dx.shape == (0, 333) and not dw.any() and not db.any()
+
+
+def test_same_bits_every_time_and_a_row_alone():
+    from paper_2604_09975_amd import clear as K
+    x, w, b, dy = inputs(5000, 1280, torch.float16, 4)
+    y, m, r = K.ckks_clear_layer_norm(x, w, b)
+    one = K.ckks_clear_layer_norm_grad(dy, x, m, r, w)
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(one, K.ckks_clear_layer_norm_grad(dy, x, m, r, w)))
+    y1, _, _ = K.ckks_clear_layer_norm(x[777:778], w, b)
+    assert torch.equal(y1, y[777:778])
+
+
+def test_rows_that_are_constant_infinite_or_not_numbers():
+    from paper_2604_09975_amd import clear as K
+    x, w, b, dy = inputs(6, 900, torch.float32, 5)
+    x[1] = 3.0                       # no deviation: y = bias
+    x[2, 5] = float("inf")
+    x[3, 899] = float("nan")
+    y, m, r = K.ckks_clear_layer_norm(x, w, b)
+    assert torch.equal(y[1], b) and r[1].item() == pytest.approx(1e-5**-0.5, rel=1e-6)
+    assert torch.isnan(y[3]).all() and torch.isnan(y[2]).any()
+    want, *_ = norm_ref(x[[0, 4, 5]], w, b, 1e-5)
+    close(y[[0, 4, 5]], want, torch.full_like(want, 1e-4), "the other rows")
+
+
+@pytest.mark.parametrize("cols", [40, 900, 3000])
+def test_gradient_against_differences(cols):
+    """Along random directions: (L(p + h v) - L(p - h v)) / 2h of L = sum(dy * y) in 64 bits.  The third derivative of a layer
+    norm of deviation about 1 makes that good to h^2; the gradient itself is a 32-bit result."""
+    from paper_2604_09975_amd import clear as K
+    g = gen(cols)
+    x, w, b, dy = randn(g, 7, cols), 1 + 0.3 * randn(g, cols), randn(g, cols), randn(g, 7, cols)
+    y, m, r = K.ckks_clear_layer_norm(x, w, b)
+    dx, dw, db = K.ckks_clear_layer_norm_grad(dy, x, m, r, w)
+    h = 1e-4
+
+    def loss(x, w, b):
+        return (dy.double() * norm_ref(x, w, b, 1e-5)[0]).sum()
+    vx, vw, vb = (randn(g, *t.shape).double() for t in (x, w, b))
+    xd, wd, bd = x.double(), w.double(), b.double()
+    for grad, v, up, down in ((dx, vx, loss(xd + h * vx, wd, bd), loss(xd - h * vx, wd, bd)),
+                              (dw, vw, loss(xd, wd + h * vw, bd), loss(xd, wd - h * vw, bd)),
+                              (db, vb, loss(xd, wd, bd + h * vb), loss(xd, wd, bd - h * vb))):
+        want, got = (up - down) / (2 * h), (grad.double() * v).sum()
+        size = (grad.double() * v).norm()
+        assert abs(want - got) <= 1e-4 * size + 1e-6 * (dy.double().abs() * y.double().abs()).sum() * 2.0**-6
+
+
+def test_refusals():
+    from paper_2604_09975_amd import binding as B
+    from paper_2604_09975_amd import clear as K
+    x, w, b, dy = inputs(4, 64, torch.float16, 6)
+    y, m, r = K.ckks_clear_layer_norm(x, w, b)
+    with pytest.raises(B.CkksError):
+        K.ckks_clear_layer_norm(x, w, b, eps=-1.0)
+    with pytest.raises(B.CkksError):
+        K.ckks_clear_layer_norm(x, w, b, eps=float("nan"))
+    with pytest.raises(ValueError):
+        K.ckks_clear_layer_norm(x, w[:63], b)
+    with pytest.raises(ValueError):
+        K.ckks_clear_layer_norm(x.t(), None, None)
+    with pytest.raises(TypeError):
+        K.ckks_clear_layer_norm(x.double(), w, b)
+    with pytest.raises(TypeError):
+        K.ckks_clear_layer_norm(x, w, b.half())
+    with pytest.raises(TypeError):
+        K.ckks_clear_layer_norm(x.cpu(), w, b)
+    with pytest.raises(TypeError):
+        K.ckks_clear_layer_norm(x, w, b, out=torch.empty(4, 64, device="cuda"))
+    with pytest.raises(B.CkksError):
+        K.ckks_clear_layer_norm(x[:1].expand(4, 64).contiguous(), w, b, out=torch.empty(1, 64, dtype=torch.float16, device="cuda").expand(4, 64))
+    with pytest.raises(ValueError):
+        K.ckks_clear_layer_norm_grad(dy[:3], x, m, r, w)
+    with pytest.raises(ValueError):
+        K.ckks_clear_layer_norm_grad(dy, x, m[:3], r, w)
+    with pytest.raises(B.CkksError):
+        K.ckks_clear_layer_norm_grad(dy, x, m, r, w, dx=x)

@@ -30,8 +30,10 @@ struct AttendArgs {
     float *lse, *part, *part_lse;
     i64 qs[2], os[2], ks[3], vs[3], ts;
     const int32_t *q_start, *kv_len, *table;
-    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, group, head_dim, window, causal;
+    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, group, head_dim, causal;
+    int window;
     int32_t page_shift;  // log2 of page_size, or -1
+    u32 whole_rows;      // page_size is a multiple of 16, and a token's stride small enough for 32-bit offsets
     u32 tiles, splits, min_tiles;
     float c;             // scale * log2(e)
 };
@@ -92,24 +94,24 @@ __device__ __forceinline__ typename Frag<T>::type col_frag(const T *v, u32 lane)
 // What a tile of rows works on.
 struct RowTile {
     u32 seq, start, n, first_row, rows;  // first token and tokens of the sequence; first row of the tile, rows in all
-    i64 kv, t0;                          // keys, position of the sequence's first new token
+    int kv, t0;                          // keys, position of the sequence's first new token
     u32 tile0, n_tiles, per, n_splits;   // first key tile, key tiles, key tiles of a split, splits
 };
 
-__device__ __forceinline__ i64 row_pos(const AttendArgs &a, const RowTile &r, u32 row) { return r.t0 + row / a.group; }
+// Position of a row; those before the cache are all alike.
+__device__ __forceinline__ int row_pos(const AttendArgs &a, const RowTile &r, u32 row) { return max(r.t0 + (int)(row / a.group), -1); }
 
 // Key tiles that the rows first_row .. first_row + ROWS - 1 see between them.
 template <int ROWS, int TK>
 __device__ __forceinline__ void key_range(const AttendArgs &a, RowTile &r) {
-    const i64 cap = (i64)a.table_width * a.page_size;
-    r.kv = max((i64)0, min((i64)a.kv_len[r.seq], cap));
-    r.t0 = (i64)a.kv_len[r.seq] - r.n;
-    if ((i64)a.kv_len[r.seq] > cap) r.t0 = cap - r.n;
+    const int kv = min(a.kv_len[r.seq], (int)(a.table_width * a.page_size));
+    r.kv = max(0, kv);
+    r.t0 = max(kv, 0) - (int)r.n;
     const u32 last = min(r.first_row + ROWS, r.rows) - 1;
-    const i64 hi = a.causal ? min(r.kv, row_pos(a, r, last) + 1) : r.kv;
-    const i64 lo = a.window ? max((i64)0, row_pos(a, r, r.first_row) - a.window + 1) : 0;
-    r.tile0 = (u32)(lo / TK);
-    r.n_tiles = hi > lo ? (u32)((hi + TK - 1) / TK) - r.tile0 : 0;
+    const int hi = a.causal ? min(r.kv, row_pos(a, r, last) + 1) : r.kv;
+    const int lo = a.window ? max(0, row_pos(a, r, r.first_row) - a.window + 1) : 0;
+    r.tile0 = (u32)lo / TK;
+    r.n_tiles = hi > lo ? ((u32)hi + TK - 1) / TK - r.tile0 : 0;
     r.per = max(a.min_tiles, (r.n_tiles + a.splits - 1) / a.splits);
     r.n_splits = max(1u, (r.n_tiles + r.per - 1) / r.per);
 }
@@ -196,12 +198,12 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     const u32 row0 = r.first_row + 32 * rw;
     const bool idle = row0 >= r.rows;                  // no row of this wave exists
     const u32 row = min(row0 + (lane & 31), r.rows - 1), token = row / a.group, head = kv_head * a.group + row % a.group;
-    const i64 pos = r.t0 + token;
-    const i64 hi = a.causal ? min(r.kv, pos + 1) : r.kv, lo = a.window ? pos - a.window + 1 : 0;  // keys lo <= j < hi are seen
+    const int pos = max(r.t0 + (int)token, -1);
+    const int hi = a.causal ? min(r.kv, pos + 1) : r.kv, lo = a.window ? pos - a.window + 1 : 0;  // keys lo <= j < hi are seen
     // bounds over the wave's rows: keys that all of them see, keys that any of them sees
-    const i64 p_first = row_pos(a, r, min(row0, r.rows - 1)), p_last = row_pos(a, r, min(row0 + 31, r.rows - 1));
-    const i64 all_hi = a.causal ? min(r.kv, p_first + 1) : r.kv, any_hi = a.causal ? min(r.kv, p_last + 1) : r.kv;
-    const i64 all_lo = a.window ? p_last - a.window + 1 : 0, any_lo = a.window ? p_first - a.window + 1 : 0;
+    const int p_first = row_pos(a, r, min(row0, r.rows - 1)), p_last = row_pos(a, r, min(row0 + 31, r.rows - 1));
+    const int all_hi = a.causal ? min(r.kv, p_first + 1) : r.kv, any_hi = a.causal ? min(r.kv, p_last + 1) : r.kv;
+    const int all_lo = a.window ? p_last - a.window + 1 : 0, any_lo = a.window ? p_first - a.window + 1 : 0;
 
     frag qf[DP / 16];
     {
@@ -221,33 +223,56 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     // a lane's piece of each row that it fetches
     const u32 stager = RW > 1 ? threadIdx.x : lane, piece = stager % PIECES, fetch_row = stager / PIECES;
     const bool piece_ok = piece * E < a.head_dim;
-    const T *kp = (const T *)a.k + (i64)kv_head * a.ks[1] + piece * E, *vp = (const T *)a.v + (i64)kv_head * a.vs[1] + piece * E;
+    const T *kp = (const T *)a.k + (i64)kv_head * a.ks[1], *vp = (const T *)a.v + (i64)kv_head * a.vs[1];
     const int32_t *table = a.table + (i64)r.seq * a.ts;
     typedef uint4 piece_t;
     piece_t kr[PASSES], vr[PASSES];
-    int32_t page;     // of key `lane` of the tile to be fetched next (lanes below TK)
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
+    int page;         // of key `lane` of the tile to be fetched next (lanes below TK); -1: none
     u32 page_row;
     auto look_up = [&](u32 tile) {
-        const i64 j = (i64)(r.tile0 + tile) * TK + (lane & (TK - 1));
+        const u32 j = (r.tile0 + tile) * TK + (lane & (TK - 1));
         page = -1;
         page_row = 0;
-        if (tile < last && j < r.kv) {
-            const u32 at = a.page_shift >= 0 ? (u32)j >> a.page_shift : (u32)j / a.page_size;
-            page_row = (u32)j - at * a.page_size;
+        if (tile < last && j < (u32)r.kv) {
+            const u32 at = a.page_shift >= 0 ? j >> a.page_shift : j / a.page_size;
+            page_row = j - at * a.page_size;
             page = table[at];
             if ((u32)page >= a.n_pages) page = -1;
         }
     };
-    auto fetch = [&]() {
+    // The rows that a wave fetches at a time are neighbours, at most 8 of them from a multiple of that on: where pages hold a
+    // multiple of 16 and the keys do not end among them, they lie in one page, whose address is then a scalar.
+    static_assert(64 / PIECES <= 8, "rows of a wave's access");
+    const u32 k_off = (u32)(lane / PIECES) * (u32)a.ks[2] + piece * E, v_off = (u32)(lane / PIECES) * (u32)a.vs[2] + piece * E;
+    auto fetch = [&](u32 tile) {
+        if (a.whole_rows && ((r.tile0 + tile) + 1) * TK <= (u32)r.kv) {
+            if (piece_ok) {
+#pragma unroll
+                for (int p = 0; p < PASSES; ++p) {
+                    const u32 key = __builtin_amdgcn_readfirstlane(p * PASS + fetch_row);
+                    const int pg = __builtin_amdgcn_readlane(page, key);
+                    const u32 pr = __builtin_amdgcn_readlane(page_row, key);
+                    if (pg >= 0) {
+                        __builtin_memcpy(&kr[p], kp + (pg * a.ks[0] + pr * a.ks[2]) + k_off, 16);
+                        __builtin_memcpy(&vr[p], vp + (pg * a.vs[0] + pr * a.vs[2]) + v_off, 16);
+                    } else {
+                        kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
+                    }
+                }
+            }
+            return;
+        }
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const u32 key = p * PASS + fetch_row;
-            const int32_t pg = __shfl(page, key);
+            const int pg = __shfl(page, key);
             const u32 pr = __shfl(page_row, key);
             kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
             if (pg >= 0 && piece_ok) {
-                __builtin_memcpy(&kr[p], kp + pg * a.ks[0] + pr * a.ks[2], 16);
-                __builtin_memcpy(&vr[p], vp + pg * a.vs[0] + pr * a.vs[2], 16);
+                __builtin_memcpy(&kr[p], kp + pg * a.ks[0] + pr * a.ks[2] + piece * E, 16);
+                __builtin_memcpy(&vr[p], vp + pg * a.vs[0] + pr * a.vs[2] + piece * E, 16);
             }
         }
     };
@@ -268,7 +293,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     float m = -__builtin_inff(), l = 0.0f;  // maximum of the row's scores (kept up to 2^8, below), the lane's part of the sum
 
     auto work = [&](u32 tile, const T *buf) {
-        const i64 j0 = (i64)(r.tile0 + tile) * TK;
+        const int j0 = (int)((r.tile0 + tile) * TK);
         if (idle || j0 >= any_hi || j0 + TK <= any_lo) return;
         const bool masked = j0 + TK > all_hi || j0 < all_lo;
         f32x16 s[SUB];
@@ -280,7 +305,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
             for (int d = 0; d < DP / 16; ++d) s[u] = mma(row_frag(buf + (u * 32 + (lane & 31)) * KS + d * 16 + half * 8), qf[d], s[u]);
         }
         // accumulator i of the lane: key 8 (i / 4) + 4 half + i % 4
-        const int see_lo = (int)max((i64)-1, min((i64)TK, lo - j0)) - 4 * (int)half, see_hi = (int)max((i64)0, min((i64)TK, hi - j0)) - 4 * (int)half;
+        const int see_lo = max(lo, j0) - j0 - 4 * (int)half, see_hi = hi - j0 - 4 * (int)half;
         if (masked) {
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
@@ -318,10 +343,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
             }
         const T *vb = buf + TK * KS;
         auto weights = [&](int u, int kk) {
-            frag b;
+            f32x8 w;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) b[j] = (T)s[u][8 * kk + j];
-            return b;
+            for (int j = 0; j < 8; ++j) w[j] = s[u][8 * kk + j];
+            return __builtin_convertvector(w, frag);
         };
         if (!masked) {
 #pragma unroll
@@ -351,23 +376,26 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
                             const int key = u * 32 + kk * 16 + 8 * (j / 4) + j % 4;
                             seen[j] = (T)(key >= see_lo && key < see_hi ? 1.0f : 0.0f);
                         }
-                        frag up, down, nan;
+                        // +infinity, -infinity, NaN
+#pragma unroll 1
+                        for (int kind = 0; kind < 3; ++kind) {
+                            frag is;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float f = (float)v[j];
-                            up[j] = (T)(f > 3.402823466e38f ? 1.0f : 0.0f);
-                            down[j] = (T)(f < -3.402823466e38f ? 1.0f : 0.0f);
-                            nan[j] = (T)(f != f ? 1.0f : 0.0f);
-                            if (!(__builtin_fabsf(f) <= 3.402823466e38f)) v[j] = (T)0.0f;
+                            for (int j = 0; j < 8; ++j) {
+                                const float f = (float)v[j];
+                                is[j] = (T)((kind == 0 ? f > 3.402823466e38f : kind == 1 ? f < -3.402823466e38f : f != f) ? 1.0f : 0.0f);
+                            }
+                            const float add = kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
+                            f32x16 n;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+                            n = mma(is, seen, n);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[d][i] += n[i] > 0.0f ? add : 0.0f;
                         }
-                        f32x16 z;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-                        const f32x16 nu = mma(up, seen, z), nd = mma(down, seen, z), nn = mma(nan, seen, z);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            o[d][i] += (nu[i] > 0.0f ? __builtin_inff() : 0.0f) + (nd[i] > 0.0f ? -__builtin_inff() : 0.0f) +
-                                       (nn[i] > 0.0f ? __builtin_nanf("") : 0.0f);
+                        for (int j = 0; j < 8; ++j)
+                            if (!(__builtin_fabsf((float)v[j]) <= 3.402823466e38f)) v[j] = (T)0.0f;
                     }
                     o[d] = mma(v, b, o[d]);
                 }
@@ -377,13 +405,13 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     T *buf = (T *)lds;
     if (RW > 1) {
         look_up(first);
-        fetch();
+        fetch(first);
         look_up(first + 1);
         if (first < last) put(buf);
         for (u32 i = first; i < last; ++i) {
             __syncthreads();
             if (i + 1 < last) {
-                fetch();
+                fetch(i + 1);
                 look_up(i + 2);
             }
             work(i, buf + (i - first & 1) * Shape::TILE);
@@ -393,14 +421,14 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     } else {
         buf += kw * Shape::TILE;
         look_up(first + kw);
-        fetch();
+        fetch(first + kw);
         look_up(first + kw + KW);
         for (u32 i = first + kw; i < last; i += KW) {
             put(buf);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             if (i + KW < last) {
-                fetch();
+                fetch(i + KW);
                 look_up(i + 2 * KW);
             }
             work(i, buf);
@@ -419,11 +447,11 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         const u64 at = (u64)(r.start + token) * a.heads + head;
         if (half == 0) {
             if (split_up)
-                a.part_lse[(u64)split * a.n_tokens * a.heads + at] = lse2;
+                a.part_lse[at * a.splits + split] = lse2;
             else if (a.lse)
                 a.lse[at] = lse2 * 0.693147180559945309f;
         }
-        float *part = a.part + ((u64)split * a.n_tokens * a.heads + at) * a.head_dim;
+        float *part = a.part + (at * a.splits + split) * a.head_dim;
         T *out = (T *)a.out + (i64)(r.start + token) * a.os[0] + head * a.os[1];
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -491,8 +519,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         const u64 at = (u64)jt * a.heads + jh;
         Pack<float, 4> res = {{some ? acc.x * inv : 0.0f, some ? acc.y * inv : 0.0f, some ? acc.z * inv : 0.0f, some ? acc.w * inv : 0.0f}};
         if (split_up) {
-            if (e == 0) a.part_lse[(u64)split * a.n_tokens * a.heads + at] = lse2;
-            store_pack<4>(a.part + ((u64)split * a.n_tokens * a.heads + at) * a.head_dim + e, res);
+            if (e == 0) a.part_lse[at * a.splits + split] = lse2;
+            store_pack<4>(a.part + (at * a.splits + split) * a.head_dim + e, res);
         } else {
             if (e == 0 && a.lse) a.lse[at] = lse2 * 0.693147180559945309f;
             Pack<T, 4> y;
@@ -503,50 +531,80 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     }
 }
 
-// Joins the splits of a row: a wave per (token, head).
-template <class T, int ROWS, int TK>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-    const u64 at = (u64)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const u32 lane = threadIdx.x & 63, token = (u32)(at / a.heads), head = (u32)(at % a.heads);
-    if (token >= a.n_tokens) return;
+// Joins the splits of a row (token, head): WAVES waves for each, a group of `lanes` lanes (four entries each) takes every
+// so-manieth split, and the groups' sums are added in their order.
+template <class T, int ROWS, int TK, int WAVES>
+__global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void attend_join_kernel(AttendArgs a, u32 lanes) {
+    constexpr int PER = WAVES < 4 ? 4 / WAVES : 1;  // rows of a block
+    __shared__ __attribute__((aligned(16))) float4 acc_of[64 * WAVES * PER];
+    __shared__ float sum_of[4 * WAVES * PER];
+    const u64 at = (u64)blockIdx.x * PER + threadIdx.x / (64 * WAVES);
+    const u32 in_row = threadIdx.x % (64 * WAVES), lane = threadIdx.x & 63;
+    const u32 token = (u32)(at / a.heads), head = (u32)(at % a.heads);
+    const u32 groups = 64 * WAVES / lanes, group = in_row / lanes, e = in_row % lanes * 4;
     RowTile r;
-    u32 lo = 0, hi = a.n_seq;
-    while (hi - lo > 1) {
-        const u32 mid = (lo + hi) >> 1;
-        if ((i64)a.q_start[mid] <= (i64)token)
-            lo = mid;
-        else
-            hi = mid;
+    r.n_splits = 1;
+    if (token < a.n_tokens) {
+        u32 lo = 0, hi = a.n_seq;
+        while (hi - lo > 1) {
+            const u32 mid = (lo + hi) >> 1;
+            if ((i64)a.q_start[mid] <= (i64)token)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        const int s = min(max(a.q_start[lo], 0), (int)a.n_tokens), end = max(min(a.q_start[lo + 1], (int)a.n_tokens), s);
+        if ((int)token >= s && (int)token < end) {
+            r.seq = lo;
+            r.start = s;
+            r.n = end - s;
+            r.rows = r.n * a.group;
+            r.first_row = ((token - s) * a.group + head % a.group) / ROWS * ROWS;
+            key_range<ROWS, TK>(a, r);
+        }
     }
-    const int s = min(max(a.q_start[lo], 0), (int)a.n_tokens), e = max(min(a.q_start[lo + 1], (int)a.n_tokens), s);
-    if ((int)token < s || (int)token >= e) return;
-    r.seq = lo;
-    r.start = s;
-    r.n = e - s;
-    r.rows = r.n * a.group;
-    r.first_row = ((token - s) * a.group + head % a.group) / ROWS * ROWS;
-    key_range<ROWS, TK>(a, r);
-    if (r.n_splits <= 1) return;  // the row has been written
-    const u64 step = (u64)a.n_tokens * a.heads;
+    // one split: the row has been written already
+    const u32 n = r.n_splits > 1 ? r.n_splits : 0;
+    const float *lse = a.part_lse + at * a.splits;
     float top = -__builtin_inff();
-    for (u32 i = 0; i < r.n_splits; ++i) top = fmaxf(top, a.part_lse[i * step + at]);
-    float sum = 0.0f, acc[4] = {0, 0, 0, 0};
-    for (u32 i = 0; i < r.n_splits; ++i) {
-        const float z = a.part_lse[i * step + at];
-        if (z == -__builtin_inff()) continue;
-        const float f = z != z ? 1.0f : __builtin_amdgcn_exp2f(z - top);
-        sum += z != z ? z : f;
-        const float *p = a.part + (i * step + at) * a.head_dim;
+    for (u32 i = lane; i < n; i += 64) top = fmaxf(top, lse[i]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k * 64 + lane < a.head_dim) acc[k] = __builtin_fmaf(f, p[k * 64 + lane], acc[k]);
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float sum = 0.0f;
+    float4 acc = make_float4(0, 0, 0, 0);
+    if (e < a.head_dim) {
+        const float *p = a.part + at * a.splits * a.head_dim + e;
+#pragma unroll 4
+        for (u32 i = group; i < n; i += groups) {
+            const float z = lse[i];
+            const float4 x = *(const float4 *)(p + (u64)i * a.head_dim);
+            // a split that saw no key has nothing to add; one whose sum is not a number has
+            const float f = z == -__builtin_inff() ? 0.0f : z != z ? z : __builtin_amdgcn_exp2f(z - top);
+            sum += f;
+            acc.x = __builtin_fmaf(f, x.x, acc.x);
+            acc.y = __builtin_fmaf(f, x.y, acc.y);
+            acc.z = __builtin_fmaf(f, x.z, acc.z);
+            acc.w = __builtin_fmaf(f, x.w, acc.w);
+        }
     }
+    acc_of[threadIdx.x] = acc;
+    if (e == 0) sum_of[threadIdx.x / lanes] = sum;
+    __syncthreads();
+    if (!n || group || e >= a.head_dim) return;
+    for (u32 g = 1; g < groups; ++g) {
+        const float4 x = acc_of[threadIdx.x + g * lanes];
+        acc.x += x.x;
+        acc.y += x.y;
+        acc.z += x.z;
+        acc.w += x.w;
+    }
+    sum = 0.0f;
+    for (u32 g = 0; g < groups; ++g) sum += sum_of[threadIdx.x / lanes + g];
     const bool some = sum > 0.0f || sum != sum;
-    if (a.lse && lane == 0) a.lse[at] = some ? (top + __log2f(sum)) * 0.693147180559945309f : -__builtin_inff();
-    T *out = (T *)a.out + (i64)token * a.os[0] + head * a.os[1];
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (k * 64 + lane < a.head_dim) out[k * 64 + lane] = (T)(some ? acc[k] / sum : 0.0f);
+    const float inv = some ? 1.0f / sum : 0.0f;
+    if (a.lse && e == 0) a.lse[at] = some ? (top + __log2f(sum)) * 0.693147180559945309f : -__builtin_inff();
+    Pack<T, 4> y = {{(T)(some ? acc.x * inv : 0.0f), (T)(some ? acc.y * inv : 0.0f), (T)(some ? acc.z * inv : 0.0f), (T)(some ? acc.w * inv : 0.0f)}};
+    store_pack<4>((T *)a.out + (i64)token * a.os[0] + head * a.os[1] + e, y);
 }
 
 // ---- host ----
@@ -579,7 +637,8 @@ static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
     // A split has 512 keys at least.  Eight blocks for each CU: sequences of different lengths then even out.
     n.min_tiles = 512 / tk;
     const u64 most = std::max<u64>(1, keys / 512);
-    n.splits = (u32)std::min<u64>(most, blocks >= 2048 ? 1 : (2048 + blocks - 1) / blocks);
+    const u64 want = n.wide ? 512 : 2048;
+    n.splits = (u32)std::min<u64>(most, blocks >= want ? 1 : (want + blocks - 1) / blocks);
     if (tiles * g.kv_heads * n.splits >= 1u << 31) return false;
     n.tiles = (u32)tiles;
     n.work_bytes = n.splits > 1 ? (u64)n.splits * b.n_tokens * p.heads * (g.head_dim + 1) * 4 : 0;
@@ -591,7 +650,14 @@ static int launch_attend(const AttendArgs &a, hipStream_t st) {
     hipLaunchKernelGGL((attend_kernel<T, DP, RW, KW, TK, OCC>), dim3(a.kv_heads * a.splits * a.tiles), dim3(64 * RW * KW), 0, st, a);
     CKKS_LAUNCH_CHECK("attend_kernel");
     if (a.splits > 1) {
-        hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK>), dim3((u32)(((u64)a.n_tokens * a.heads + 3) / 4)), dim3(256), 0, st, a);
+        const u64 rows = (u64)a.n_tokens * a.heads;
+        const u32 lanes = DP / 4;
+        if (a.splits <= 8)
+            hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK, 1>), dim3((u32)((rows + 3) / 4)), dim3(256), 0, st, a, lanes);
+        else if (a.splits <= 32)
+            hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK, 4>), dim3((u32)rows), dim3(256), 0, st, a, lanes);
+        else
+            hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK, 16>), dim3((u32)rows), dim3(1024), 0, st, a, lanes);
         CKKS_LAUNCH_CHECK("attend_join_kernel");
     }
     return CKKS_OK;
@@ -677,8 +743,11 @@ int ckks_clear_attend(const ckks_clear_attend_t *p, void *stream) {
     a.ts = b.table_stride, a.q_start = b.d_q_start, a.kv_len = b.d_kv_len, a.table = b.d_page_table;
     a.n_seq = b.n_seq, a.n_tokens = b.n_tokens, a.n_pages = g.n_pages, a.page_size = g.page_size, a.table_width = b.table_width;
     a.kv_heads = g.kv_heads, a.heads = p->heads, a.group = p->heads / g.kv_heads, a.head_dim = g.head_dim;
-    a.window = p->window, a.causal = p->flags & CKKS_CLEAR_CAUSAL;
+    // a window of all positions is none
+    a.window = p->window < (u64)b.table_width * g.page_size ? (int)p->window : 0, a.causal = p->flags & CKKS_CLEAR_CAUSAL;
     a.page_shift = (g.page_size & (g.page_size - 1)) ? -1 : 31 - __builtin_clz(g.page_size);
+    const auto near = [](i64 stride) { return stride >= 0 && stride < 1 << 24; };
+    a.whole_rows = g.page_size % 16 == 0 && near(g.k_stride[2]) && near(g.v_stride[2]);
     a.tiles = n.tiles, a.splits = n.splits, a.min_tiles = n.min_tiles;
     a.c = p->scale * 1.44269504088896340736f;
     hipStream_t st = (hipStream_t)stream;

@@ -12,6 +12,7 @@
 // Either may split the keys over several blocks; a second kernel then joins the blocks' results in order.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "clear_device.h"
 
@@ -33,7 +34,7 @@ struct AttendArgs {
     u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, group, head_dim, causal;
     int window;
     int32_t page_shift;  // log2 of page_size, or -1
-    u32 whole_rows;      // page_size is a multiple of 16, and a token's stride small enough for 32-bit offsets
+    u32 whole_rows;      // page_size is a multiple of 16, and offsets within a page fit 32 bits
     u32 tiles, splits, min_tiles;
     float c;             // scale * log2(e)
 };
@@ -135,13 +136,13 @@ __device__ __forceinline__ bool find_tile(const AttendArgs &a, u32 tile, RowTile
             const u32 up = __shfl_up(sum, o);
             if (lane >= (u32)o) sum += up;
         }
-        const u32 total = __shfl(sum, 63);
+        const u32 total = __builtin_amdgcn_readlane(sum, 63);
         if (tile - before < total) {
             const int at = __ffsll((unsigned long long)__ballot(sum > tile - before)) - 1;
             r.seq = base + at;
-            r.start = __shfl(s, at);
-            r.n = __shfl(e, at) - r.start;
-            r.first_row = (tile - before - (__shfl(sum, at) - __shfl(tiles, at))) * ROWS;
+            r.start = __builtin_amdgcn_readlane(s, at);
+            r.n = __builtin_amdgcn_readlane(e, at) - r.start;
+            r.first_row = (tile - before - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(tiles, at))) * ROWS;
             r.rows = r.n * a.group;
             return true;
         }
@@ -150,15 +151,23 @@ __device__ __forceinline__ bool find_tile(const AttendArgs &a, u32 tile, RowTile
     return false;
 }
 
+__device__ __forceinline__ bool is_finite(float x) { return __builtin_fabsf(x) <= 3.402823466e38f; }
+// 16 bytes of T with zeros in place of infinities and NaN, whose exponents are all ones; `odd` becomes nonzero if there was one.
 template <class T>
-__device__ __forceinline__ u32 not_finite(typename Frag<T>::type x) {
-    u32 bad = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float f = (float)x[j];
-        bad |= !(__builtin_fabsf(f) <= 3.402823466e38f);
-    }
-    return bad;
+__device__ __forceinline__ uint4 finite_part(uint4 x, u32 &odd) {
+    auto clean = [&](u32 w) {
+        if constexpr (sizeof(T) == 4) {
+            const u32 bad = (w & 0x7f800000u) == 0x7f800000u ? ~0u : 0u;
+            odd |= bad;
+            return w & ~bad;
+        } else {
+            constexpr u32 EXP = std::is_same<T, f16>::value ? 0x7c007c00u : 0x7f807f80u, ONE = EXP & (0u - EXP) & 0xffffu;
+            const u32 top = (w & EXP) + ONE * 0x10001u & 0x80008000u;  // both halves at once: the sum of a half stays in it
+            odd |= top;
+            return w & ~(top | (top - (top >> 15)));
+        }
+    };
+    return make_uint4(clean(x.x), clean(x.y), clean(x.z), clean(x.w));
 }
 
 template <class T, int DP, int RW, int KW, int TK>
@@ -185,12 +194,19 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     constexpr int PASSES = TK / PASS;
     __shared__ __attribute__((aligned(16))) unsigned char lds[Shape::LDS];
 
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const u32 kv_head = blockIdx.x % a.kv_heads, split = blockIdx.x / a.kv_heads % a.splits;
     RowTile r;
     // the last tiles of a causal chunk see the most keys: they start first
     if (!find_tile<ROWS>(a, a.tiles - 1 - blockIdx.x / a.kv_heads / a.splits, r)) return;
     key_range<ROWS, TK>(a, r);
+    // the same in every lane: scalars from here on
+    r.kv = __builtin_amdgcn_readfirstlane(r.kv);
+    r.t0 = __builtin_amdgcn_readfirstlane(r.t0);
+    r.tile0 = __builtin_amdgcn_readfirstlane(r.tile0);
+    r.n_tiles = __builtin_amdgcn_readfirstlane(r.n_tiles);
+    r.per = __builtin_amdgcn_readfirstlane(r.per);
+    r.n_splits = __builtin_amdgcn_readfirstlane(r.n_splits);
     if (split >= r.n_splits) return;
     const u32 first = split * r.per, last = min(first + r.per, r.n_tiles);
 
@@ -203,6 +219,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     // bounds over the wave's rows: keys that all of them see, keys that any of them sees
     const int p_first = row_pos(a, r, min(row0, r.rows - 1)), p_last = row_pos(a, r, min(row0 + 31, r.rows - 1));
     const int all_hi = a.causal ? min(r.kv, p_first + 1) : r.kv, any_hi = a.causal ? min(r.kv, p_last + 1) : r.kv;
+    // ... of the block's rows
+    const int block_hi = a.causal ? min(r.kv, row_pos(a, r, r.first_row) + 1) : r.kv,
+              block_lo = a.window ? row_pos(a, r, min(r.first_row + ROWS, r.rows) - 1) - a.window + 1 : 0;
     const int all_lo = a.window ? p_last - a.window + 1 : 0, any_lo = a.window ? p_first - a.window + 1 : 0;
 
     frag qf[DP / 16];
@@ -229,60 +248,88 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     piece_t kr[PASSES], vr[PASSES];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
-    int page;         // of key `lane` of the tile to be fetched next (lanes below TK); -1: none
-    u32 page_row;
+    struct Place {
+        int page;     // of key `lane` of a tile (lanes below TK) as the table has it; -1: none
+        u32 row;
+    };
     auto look_up = [&](u32 tile) {
         const u32 j = (r.tile0 + tile) * TK + (lane & (TK - 1));
-        page = -1;
-        page_row = 0;
+        Place at{-1, 0};
         if (tile < last && j < (u32)r.kv) {
-            const u32 at = a.page_shift >= 0 ? j >> a.page_shift : j / a.page_size;
-            page_row = j - at * a.page_size;
-            page = table[at];
-            if ((u32)page >= a.n_pages) page = -1;
+            const u32 n = a.page_shift >= 0 ? j >> a.page_shift : j / a.page_size;
+            at.row = j - n * a.page_size;
+            at.page = table[n];  // looked at only where it is used: a wait here would be one for all loads under way
         }
+        return at;
     };
     // The rows that a wave fetches at a time are neighbours, at most 8 of them from a multiple of that on: where pages hold a
     // multiple of 16 and the keys do not end among them, they lie in one page, whose address is then a scalar.
+    // Rows and pieces that are not there are fetched from page 0 and become zeros when they are put into LDS (`none`: a bit
+    // for each pass): a branch around a load would have its result copied, and so waited for, at once.
     static_assert(64 / PIECES <= 8, "rows of a wave's access");
-    const u32 k_off = (u32)(lane / PIECES) * (u32)a.ks[2] + piece * E, v_off = (u32)(lane / PIECES) * (u32)a.vs[2] + piece * E;
-    auto fetch = [&](u32 tile) {
-        if (a.whole_rows && ((r.tile0 + tile) + 1) * TK <= (u32)r.kv) {
-            if (piece_ok) {
+    const u32 lane_piece = piece_ok ? piece * E : 0;
+    auto fetch = [&](u32 tile, const Place &at, const T *base, const i64 *stride, piece_t *to) {
+        u32 none = piece_ok ? 0 : ~0u;
+        u64 src[PASSES];
+        if (a.whole_rows && (r.tile0 + tile + 1) * TK <= (u32)r.kv) {
+            const u32 off = (lane / PIECES) * (u32)stride[2] + lane_piece;
 #pragma unroll
-                for (int p = 0; p < PASSES; ++p) {
-                    const u32 key = __builtin_amdgcn_readfirstlane(p * PASS + fetch_row);
-                    const int pg = __builtin_amdgcn_readlane(page, key);
-                    const u32 pr = __builtin_amdgcn_readlane(page_row, key);
-                    if (pg >= 0) {
-                        __builtin_memcpy(&kr[p], kp + (pg * a.ks[0] + pr * a.ks[2]) + k_off, 16);
-                        __builtin_memcpy(&vr[p], vp + (pg * a.vs[0] + pr * a.vs[2]) + v_off, 16);
-                    } else {
-                        kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
-                    }
+            for (int p = 0; p < PASSES; ++p) {
+                const u32 key = __builtin_amdgcn_readfirstlane(p * PASS + fetch_row);
+                u32 pg = __builtin_amdgcn_readlane(at.page, key);
+                const u32 pr = __builtin_amdgcn_readlane(at.row, key);
+                if (pg >= a.n_pages) {
+                    pg = 0;
+                    none |= 1u << p;
                 }
+                src[p] = (u64)pg * stride[0] + (pr * (u32)stride[2] + off);
             }
-            return;
-        }
+        } else {
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const u32 key = p * PASS + fetch_row;
-            const int pg = __shfl(page, key);
-            const u32 pr = __shfl(page_row, key);
-            kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
-            if (pg >= 0 && piece_ok) {
-                __builtin_memcpy(&kr[p], kp + pg * a.ks[0] + pr * a.ks[2] + piece * E, 16);
-                __builtin_memcpy(&vr[p], vp + pg * a.vs[0] + pr * a.vs[2] + piece * E, 16);
+            for (int p = 0; p < PASSES; ++p) {
+                const u32 key = p * PASS + fetch_row;
+                u32 pg = __shfl(at.page, key);
+                const u32 pr = __shfl(at.row, key);
+                if (pg >= a.n_pages) {
+                    pg = 0;
+                    none |= 1u << p;
+                }
+                src[p] = (u64)pg * stride[0] + pr * stride[2] + lane_piece;
             }
         }
+        if (a.n_pages)
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) __builtin_memcpy(&to[p], base + src[p], 16);
+        return none;
     };
-    auto put = [&](T *buf) {
+    u32 k_none = 0, v_none = 0;
+    auto fetch_k = [&](u32 tile, const Place &at) { k_none = fetch(tile, at, kp, a.ks, kr); };
+    auto fetch_v = [&](u32 tile, const Place &at) { v_none = fetch(tile, at, vp, a.vs, vr); };
+    auto blank = [&](piece_t *x, u32 none) {
+        if (__any(none != 0))
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const u32 key = p * PASS + fetch_row;
-            *(piece_t *)(buf + key * KS + piece * E) = kr[p];
-            *(piece_t *)(buf + TK * KS + key * VS + piece * E) = vr[p];
-        }
+            for (int p = 0; p < PASSES; ++p)
+                if (none >> p & 1) x[p] = make_uint4(0, 0, 0, 0);
+    };
+    auto put_k = [&](T *buf) {
+        blank(kr, k_none);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) *(piece_t *)(buf + (p * PASS + fetch_row) * KS + piece * E) = kr[p];
+    };
+    // A weight of 0 does not keep an infinity or NaN of an unseen value out of a sum.  In a tile that some row of the block does
+    // not see in full such values are taken as zeros; whether there were any decides about the pass at the end.
+    u32 odd = 0;
+    auto partial = [&](u32 tile) {
+        const int j0 = (int)((r.tile0 + tile) * TK);
+        return j0 + TK > block_hi || j0 < block_lo;
+    };
+    auto put_v = [&](u32 tile, T *buf) {
+        blank(vr, v_none);
+        if (partial(tile))
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) vr[p] = finite_part<T>(vr[p], odd);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) *(piece_t *)(buf + (p * PASS + fetch_row) * VS + piece * E) = vr[p];
     };
 
     f32x16 o[DT];
@@ -292,27 +339,39 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -__builtin_inff(), l = 0.0f;  // maximum of the row's scores (kept up to 2^8, below), the lane's part of the sum
 
-    auto work = [&](u32 tile, const T *buf) {
+    f32x16 s[SUB];       // scores of a tile; accumulator i of a lane: key 8 (i / 4) + 4 half + i % 4 of its 32
+    frag w[2 * SUB];     // weights, 16 keys each
+    // whether any row of the wave sees the tile, and whether some row does not see all of it
+    auto seen = [&](u32 tile) {
         const int j0 = (int)((r.tile0 + tile) * TK);
-        if (idle || j0 >= any_hi || j0 + TK <= any_lo) return;
-        const bool masked = j0 + TK > all_hi || j0 < all_lo;
-        f32x16 s[SUB];
+        return !idle && j0 < any_hi && j0 + TK > any_lo;
+    };
+    auto masked = [&](u32 tile) {
+        const int j0 = (int)((r.tile0 + tile) * TK);
+        return j0 + TK > all_hi || j0 < all_lo;
+    };
+    auto see_lo = [&](u32 tile) { return lo - (int)((r.tile0 + tile) * TK) - 4 * (int)half; };
+    auto see_hi = [&](u32 tile) { return hi - (int)((r.tile0 + tile) * TK) - 4 * (int)half; };
+
+    auto score = [&](const T *kb) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u) {
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) s[u] = mma(row_frag(buf + (u * 32 + (lane & 31)) * KS + d * 16 + half * 8), qf[d], s[u]);
-        }
-        // accumulator i of the lane: key 8 (i / 4) + 4 half + i % 4
-        const int see_lo = max(lo, j0) - j0 - 4 * (int)half, see_hi = hi - j0 - 4 * (int)half;
-        if (masked) {
+        for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) s[u] = mma(row_frag(kb + (u * 32 + (lane & 31)) * KS + d * 16 + half * 8), qf[d], s[u]);
+    };
+    auto soften = [&](u32 tile) {
+        if (masked(tile)) {
+            const int from = see_lo(tile), to = see_hi(tile);
 #pragma unroll
             for (int u = 0; u < SUB; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = u * 32 + 8 * (i / 4) + i % 4;
-                    if (key < see_lo || key >= see_hi) s[u][i] = -__builtin_inff();
+                    if (key < from || key >= to) s[u][i] = -__builtin_inff();
                 }
         }
         float top = s[0][0];
@@ -334,102 +393,123 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
         const float mc = m == -__builtin_inff() ? 0.0f : m * a.c;
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 s[u][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.c, -mc));
-                l += s[u][i];
+                sum[i % 4] += s[u][i];
             }
-        const T *vb = buf + TK * KS;
-        auto weights = [&](int u, int kk) {
-            f32x8 w;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = s[u][8 * kk + j];
-            return __builtin_convertvector(w, frag);
-        };
-        if (!masked) {
-#pragma unroll
-            for (int u = 0; u < SUB; ++u)
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    const frag b = weights(u, kk);
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[d] = mma(col_frag<T, VS>(vb + (u * 32 + kk * 16) * VS + d * 32, lane), b, o[d]);
-                }
-            return;
-        }
-        // A weight of 0 does not keep an infinity or NaN of an unseen value out of a sum.  Where a tile has one, the rows
-        // that see it are counted by further products, and only those take it in.
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
-                const frag b = weights(u, kk);
+                f32x8 x;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    frag v = col_frag<T, VS>(vb + (u * 32 + kk * 16) * VS + d * 32, lane);
-                    if (__any(not_finite<T>(v))) {
-                        frag seen;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const int key = u * 32 + kk * 16 + 8 * (j / 4) + j % 4;
-                            seen[j] = (T)(key >= see_lo && key < see_hi ? 1.0f : 0.0f);
-                        }
-                        // +infinity, -infinity, NaN
-#pragma unroll 1
-                        for (int kind = 0; kind < 3; ++kind) {
-                            frag is;
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float f = (float)v[j];
-                                is[j] = (T)((kind == 0 ? f > 3.402823466e38f : kind == 1 ? f < -3.402823466e38f : f != f) ? 1.0f : 0.0f);
-                            }
-                            const float add = kind == 0 ? __builtin_inff() : kind == 1 ? -__builtin_inff() : __builtin_nanf("");
-                            f32x16 n;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) n[i] = 0.0f;
-                            n = mma(is, seen, n);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[d][i] += n[i] > 0.0f ? add : 0.0f;
-                        }
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (!(__builtin_fabsf((float)v[j]) <= 3.402823466e38f)) v[j] = (T)0.0f;
-                    }
-                    o[d] = mma(v, b, o[d]);
-                }
+                for (int j = 0; j < 8; ++j) x[j] = s[u][8 * kk + j];
+                w[2 * u + kk] = __builtin_convertvector(x, frag);
             }
+    };
+    auto gather = [&](const T *vb) {
+#pragma unroll
+        for (int k = 0; k < 2 * SUB; ++k)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = mma(col_frag<T, VS>(vb + k * 16 * VS + d * 32, lane), w[k], o[d]);
+    };
+    auto work = [&](u32 tile, const T *buf) {
+        if (!seen(tile)) return;
+        score(buf);
+        soften(tile);
+        gather(buf + TK * KS);
     };
 
     T *buf = (T *)lds;
-    if (RW > 1) {
-        look_up(first);
-        fetch(first);
-        look_up(first + 1);
-        if (first < last) put(buf);
+    if constexpr (RW == 8) {
+        // Two sets of four waves, one of each on every SIMD, work half a tile apart: while one set keeps the matrix units busy
+        // (scores of tile i, sum of tile i - 1), the other does the softmax of its tile and moves the next one in.  A barrier
+        // ends each half.  Keys of tile i + 1 and values of tile i are written while those before them are read: two
+        // buffers of each.
+        const u32 set = wave >> 2, n = last - first;
+        T *kb = buf, *vb = buf + 2 * TK * KS;
+        auto half_done = [] {
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        Place k_at = look_up(first), v_at = k_at;
+        fetch_k(first, k_at);
+        put_k(kb);
+        fetch_v(first, v_at);
+        v_at = look_up(first + 1);
+        fetch_k(first + 1, v_at);
+        k_at = look_up(first + 2);
+        auto stage = [&](u32 i) {
+            if (i >= n) return;
+            put_k(kb + (i + 1 & 1) * TK * KS);
+            put_v(first + i, vb + (i & 1) * TK * VS);
+            fetch_v(first + i + 1, v_at);
+            fetch_k(first + i + 2, k_at);
+            v_at = k_at;
+            k_at = look_up(first + i + 3);
+        };
+        half_done();
+        if (set) {
+            stage(0);
+            half_done();
+        }
+        for (u32 i = 0; i <= n; ++i) {
+            __builtin_amdgcn_s_setprio(1);
+            const bool now = i < n && seen(first + i), before = i && seen(first + i - 1);
+            const T *ki = kb + (i & 1) * TK * KS, *vi = vb + (i + 1 & 1) * TK * VS;
+            if (now) score(ki);
+            if (before) gather(vi);
+            __builtin_amdgcn_s_setprio(0);
+            half_done();
+            if (now) soften(first + i);
+            stage(i + set);
+            half_done();
+        }
+        if (!set) half_done();
+    } else if constexpr (RW > 1) {
+        Place at = look_up(first);
+        fetch_k(first, at);
+        fetch_v(first, at);
+        at = look_up(first + 1);
+        put_k(buf);
+        put_v(first, buf + TK * KS);
         for (u32 i = first; i < last; ++i) {
             __syncthreads();
             if (i + 1 < last) {
-                fetch(i + 1);
-                look_up(i + 2);
+                fetch_k(i + 1, at);
+                fetch_v(i + 1, at);
+                at = look_up(i + 2);
             }
             work(i, buf + (i - first & 1) * Shape::TILE);
             // the other buffer was read before this round's barrier
-            if (i + 1 < last) put(buf + (i + 1 - first & 1) * Shape::TILE);
+            if (i + 1 < last) {
+                put_k(buf + (i + 1 - first & 1) * Shape::TILE);
+                put_v(i + 1, buf + (i + 1 - first & 1) * Shape::TILE + TK * KS);
+            }
         }
     } else {
         buf += kw * Shape::TILE;
-        look_up(first + kw);
-        fetch(first + kw);
-        look_up(first + kw + KW);
+        Place at = look_up(first + kw);
+        fetch_k(first + kw, at);
+        fetch_v(first + kw, at);
+        at = look_up(first + kw + KW);
         for (u32 i = first + kw; i < last; i += KW) {
-            put(buf);
+            put_k(buf);
+            put_v(i, buf + TK * KS);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             if (i + KW < last) {
-                fetch(i + KW);
-                look_up(i + 2 * KW);
+                fetch_k(i + KW, at);
+                fetch_v(i + KW, at);
+                at = look_up(i + 2 * KW);
             }
             work(i, buf);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -437,6 +517,36 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         }
     }
     l += __shfl_xor(l, 32);
+
+    // What put_v left out, added to the rows that see it: their sums take nothing else that could undo it any more.
+    const bool left_out = RW > 1 ? __syncthreads_or(odd != 0) : __any(odd != 0);
+    if (left_out) {
+#pragma unroll 1
+        for (u32 i = RW > 1 ? first : first + kw; i < last; i += KW) {
+            if (!partial(i)) continue;
+            const Place at = look_up(i);
+#pragma unroll 1
+            for (int key = 0; key < TK; ++key) {
+                const int pg = __builtin_amdgcn_readlane(at.page, key), j = (int)((r.tile0 + i) * TK) + key;
+                if ((u32)pg >= a.n_pages) continue;
+                const T *v = vp + pg * a.vs[0] + (u32)__builtin_amdgcn_readlane(at.row, key) * a.vs[2];
+#pragma unroll 1
+                for (u32 e0 = 0; e0 < a.head_dim; e0 += 64) {
+                    const float x = e0 + lane < a.head_dim ? (float)v[e0 + lane] : 0.0f;
+                    for (unsigned long long bad = __ballot(!is_finite(x)); bad; bad &= bad - 1) {
+                        const int b = __ffsll(bad) - 1;
+                        const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), b));
+                        if (j >= lo && j < hi)
+#pragma unroll
+                            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                                for (int k = 0; k < 16; ++k)
+                                    if (d * 32 + 8 * (k / 4) + 4 * (int)half + k % 4 == (int)e0 + b) o[d][k] += add;
+                    }
+                }
+            }
+        }
+    }
 
     // Result of rows in this wave (or of the block's 32 rows): O^T holds entry 32 d + 8 (i / 4) + 4 half + i % 4 of its row.
     const bool split_up = r.n_splits > 1;
@@ -627,9 +737,9 @@ static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
     n.dp = g.head_dim <= 64 ? 64 : g.head_dim <= 128 ? 128 : 256;
     const bool f32 = g.dtype == CKKS_CLEAR_F32;
     // Sharing tiles reads keys and values a quarter as often; it needs enough row tiles of 128 to fill 256 CUs.
-    const u64 wide_blocks = (rows / 128) * g.kv_heads;
-    n.wide = wide_blocks >= 256 || (f32 && n.dp == 256);
-    const u64 r = n.wide ? 128 : 32;
+    const u64 wide_rows = f32 || n.dp == 256 ? 128 : 256;
+    n.wide = rows / 128 * g.kv_heads >= 256 || (f32 && n.dp == 256);
+    const u64 r = n.wide ? wide_rows : 32;
     const u64 tiles = rows / r + seqs;                       // at most
     const u64 likely = seqs ? seqs * ((rows / seqs + r - 1) / r) : 0;
     const u64 blocks = std::max<u64>(likely * g.kv_heads, 1);
@@ -637,7 +747,7 @@ static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
     // A split has 512 keys at least.  Eight blocks for each CU: sequences of different lengths then even out.
     n.min_tiles = 512 / tk;
     const u64 most = std::max<u64>(1, keys / 512);
-    const u64 want = n.wide ? 512 : 2048;
+    const u64 want = n.wide ? (wide_rows == 256 ? 256 : 512) : 2048;
     n.splits = (u32)std::min<u64>(most, blocks >= want ? 1 : (want + blocks - 1) / blocks);
     if (tiles * g.kv_heads * n.splits >= 1u << 31) return false;
     n.tiles = (u32)tiles;
@@ -666,8 +776,8 @@ template <class T>
 static int launch_attend(const AttendArgs &a, const AttendPlan &n, hipStream_t st) {
     constexpr bool f32 = sizeof(T) == 4;
     if (n.wide) {
-        if (n.dp == 64) return launch_attend<T, 64, 4, 1, f32 ? 32 : 64, 2>(a, st);
-        if (n.dp == 128) return launch_attend<T, 128, 4, 1, f32 ? 32 : 64, f32 ? 1 : 2>(a, st);
+        if (n.dp == 64) return launch_attend<T, 64, f32 ? 4 : 8, 1, f32 ? 32 : 64, 2>(a, st);
+        if (n.dp == 128) return launch_attend<T, 128, f32 ? 4 : 8, 1, f32 ? 32 : 64, f32 ? 1 : 2>(a, st);
         return launch_attend<T, 256, 4, 1, 32, 1>(a, st);
     }
     if (n.dp == 64) return launch_attend<T, 64, 1, 4, 32, f32 ? 1 : 2>(a, st);
@@ -746,7 +856,7 @@ int ckks_clear_attend(const ckks_clear_attend_t *p, void *stream) {
     // a window of all positions is none
     a.window = p->window < (u64)b.table_width * g.page_size ? (int)p->window : 0, a.causal = p->flags & CKKS_CLEAR_CAUSAL;
     a.page_shift = (g.page_size & (g.page_size - 1)) ? -1 : 31 - __builtin_clz(g.page_size);
-    const auto near = [](i64 stride) { return stride >= 0 && stride < 1 << 24; };
+    const auto near = [&](i64 stride) { return stride >= 0 && stride < 1 << 24 && (u64)stride * g.page_size < 1u << 31; };
     a.whole_rows = g.page_size % 16 == 0 && near(g.k_stride[2]) && near(g.v_stride[2]);
     a.tiles = n.tiles, a.splits = n.splits, a.min_tiles = n.min_tiles;
     a.c = p->scale * 1.44269504088896340736f;

@@ -33,8 +33,8 @@ struct AttendArgs {
     const int32_t *q_start, *kv_len, *table;
     u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, group, head_dim, causal;
     int window;
-    int32_t page_shift;  // log2 of page_size, or -1
-    u32 whole_rows;      // page_size is a multiple of 16, and offsets within a page fit 32 bits
+    u32 page_mul, page_shift;  // position / page_size = (position * page_mul >> 32) >> page_shift; page_mul 0: a shift alone
+    u32 near, alike;           // strides of pages and offsets within one fit 32 bits; keys and values have the same strides
     u32 tiles, splits, min_tiles;
     float c;             // scale * log2(e)
 };
@@ -248,63 +248,67 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     piece_t kr[PASSES], vr[PASSES];
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
+    // Where the rows that this thread fetches lie.  The table's answer is looked at only when it is needed, a tile later: a wait
+    // or a branch here would be a wait for all loads under way.
     struct Place {
-        int page;     // of key `lane` of a tile (lanes below TK) as the table has it; -1: none
-        u32 row;
+        u32 page[PASSES], row[PASSES];
     };
     auto look_up = [&](u32 tile) {
-        const u32 j = (r.tile0 + tile) * TK + (lane & (TK - 1));
-        Place at{-1, 0};
-        if (tile < last && j < (u32)r.kv) {
-            const u32 n = a.page_shift >= 0 ? j >> a.page_shift : j / a.page_size;
-            at.row = j - n * a.page_size;
-            at.page = table[n];  // looked at only where it is used: a wait here would be one for all loads under way
+        Place at;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const u32 j = min((r.tile0 + tile) * TK + p * PASS + fetch_row, (u32)r.kv - 1);
+            const u32 n = a.page_mul ? __umulhi(j, a.page_mul) >> a.page_shift : j >> a.page_shift;
+            at.page[p] = (u32)table[n];
+            at.row[p] = j - n * a.page_size;
         }
         return at;
     };
-    // The rows that a wave fetches at a time are neighbours, at most 8 of them from a multiple of that on: where pages hold a
-    // multiple of 16 and the keys do not end among them, they lie in one page, whose address is then a scalar.
     // Rows and pieces that are not there are fetched from page 0 and become zeros when they are put into LDS (`none`: a bit
     // for each pass): a branch around a load would have its result copied, and so waited for, at once.
-    static_assert(64 / PIECES <= 8, "rows of a wave's access");
     const u32 lane_piece = piece_ok ? piece * E : 0;
-    auto fetch = [&](u32 tile, const Place &at, const T *base, const i64 *stride, piece_t *to) {
-        u32 none = piece_ok ? 0 : ~0u;
-        u64 src[PASSES];
-        if (a.whole_rows && (r.tile0 + tile + 1) * TK <= (u32)r.kv) {
-            const u32 off = (lane / PIECES) * (u32)stride[2] + lane_piece;
+    struct Sources {
+        u64 k[PASSES], v[PASSES];
+        u32 none;
+    };
+    auto locate = [&](u32 tile, const Place &at) {
+        Sources s;
+        s.none = piece_ok ? 0 : ~0u;
+        const bool ends = (r.tile0 + tile + 1) * TK > (u32)r.kv;
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) {
-                const u32 key = __builtin_amdgcn_readfirstlane(p * PASS + fetch_row);
-                u32 pg = __builtin_amdgcn_readlane(at.page, key);
-                const u32 pr = __builtin_amdgcn_readlane(at.row, key);
-                if (pg >= a.n_pages) {
-                    pg = 0;
-                    none |= 1u << p;
-                }
-                src[p] = (u64)pg * stride[0] + (pr * (u32)stride[2] + off);
+        for (int p = 0; p < PASSES; ++p) {
+            u32 pg = at.page[p];
+            if (pg >= a.n_pages) {
+                pg = 0;
+                s.none |= 1u << p;
             }
-        } else {
-#pragma unroll
-            for (int p = 0; p < PASSES; ++p) {
-                const u32 key = p * PASS + fetch_row;
-                u32 pg = __shfl(at.page, key);
-                const u32 pr = __shfl(at.row, key);
-                if (pg >= a.n_pages) {
-                    pg = 0;
-                    none |= 1u << p;
-                }
-                src[p] = (u64)pg * stride[0] + pr * stride[2] + lane_piece;
+            if (ends && (r.tile0 + tile) * TK + p * PASS + fetch_row >= (u32)r.kv) s.none |= 1u << p;
+            if (a.near) {
+                s.k[p] = (u64)pg * (u32)a.ks[0] + (at.row[p] * (u32)a.ks[2] + lane_piece);
+                s.v[p] = a.alike ? s.k[p] : (u64)pg * (u32)a.vs[0] + (at.row[p] * (u32)a.vs[2] + lane_piece);
+            } else {
+                s.k[p] = (u64)pg * a.ks[0] + (u64)at.row[p] * a.ks[2] + lane_piece;
+                s.v[p] = (u64)pg * a.vs[0] + (u64)at.row[p] * a.vs[2] + lane_piece;
             }
         }
-        if (a.n_pages)
-#pragma unroll
-            for (int p = 0; p < PASSES; ++p) __builtin_memcpy(&to[p], base + src[p], 16);
-        return none;
+        return s;
     };
     u32 k_none = 0, v_none = 0;
-    auto fetch_k = [&](u32 tile, const Place &at) { k_none = fetch(tile, at, kp, a.ks, kr); };
-    auto fetch_v = [&](u32 tile, const Place &at) { v_none = fetch(tile, at, vp, a.vs, vr); };
+    auto fetch_k = [&](const Sources &from) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) __builtin_memcpy(&kr[p], kp + from.k[p], 16);
+        k_none = from.none;
+    };
+    auto fetch_v = [&](const Sources &from) {
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) __builtin_memcpy(&vr[p], vp + from.v[p], 16);
+        v_none = from.none;
+    };
+    auto fetch = [&](u32 tile, const Place &at) {
+        const Sources from = locate(tile, at);
+        fetch_k(from);
+        fetch_v(from);
+    };
     auto blank = [&](piece_t *x, u32 none) {
         if (__any(none != 0))
 #pragma unroll
@@ -325,7 +329,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     };
     auto put_v = [&](u32 tile, T *buf) {
         blank(vr, v_none);
-        if (partial(tile))
+        if (partial(tile) && tile < last)
 #pragma unroll
             for (int p = 0; p < PASSES; ++p) vr[p] = finite_part<T>(vr[p], odd);
 #pragma unroll
@@ -426,7 +430,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     };
 
     T *buf = (T *)lds;
-    if constexpr (RW == 8) {
+    if (first >= last) {  // no key is seen: nothing may be looked up either
+    } else if constexpr (RW == 8) {
         // Two sets of four waves, one of each on every SIMD, work half a tile apart: while one set keeps the matrix units busy
         // (scores of tile i, sum of tile i - 1), the other does the softmax of its tile and moves the next one in.  A barrier
         // ends each half.  Keys of tile i + 1 and values of tile i are written while those before them are read: two
@@ -440,21 +445,22 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
             __builtin_amdgcn_sched_barrier(0);
         };
-        Place k_at = look_up(first), v_at = k_at;
-        fetch_k(first, k_at);
+        Place at = look_up(first);
+        fetch(first, at);
+        at = look_up(first + 1);
         put_k(kb);
-        fetch_v(first, v_at);
-        v_at = look_up(first + 1);
-        fetch_k(first + 1, v_at);
-        k_at = look_up(first + 2);
+        Sources next = locate(first + 1, at);
+        fetch_k(next);
+        at = look_up(first + 2);
+        // Past the last tile this moves what nobody reads.
         auto stage = [&](u32 i) {
-            if (i >= n) return;
             put_k(kb + (i + 1 & 1) * TK * KS);
             put_v(first + i, vb + (i & 1) * TK * VS);
-            fetch_v(first + i + 1, v_at);
-            fetch_k(first + i + 2, k_at);
-            v_at = k_at;
-            k_at = look_up(first + i + 3);
+            const Sources after = locate(first + i + 2, at);
+            at = look_up(first + i + 3);
+            fetch_v(next);
+            fetch_k(after);
+            next = after;
         };
         half_done();
         if (set) {
@@ -476,30 +482,25 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         if (!set) half_done();
     } else if constexpr (RW > 1) {
         Place at = look_up(first);
-        fetch_k(first, at);
-        fetch_v(first, at);
+        fetch(first, at);
         at = look_up(first + 1);
         put_k(buf);
         put_v(first, buf + TK * KS);
         for (u32 i = first; i < last; ++i) {
             __syncthreads();
             if (i + 1 < last) {
-                fetch_k(i + 1, at);
-                fetch_v(i + 1, at);
+                fetch(i + 1, at);
                 at = look_up(i + 2);
             }
             work(i, buf + (i - first & 1) * Shape::TILE);
             // the other buffer was read before this round's barrier
-            if (i + 1 < last) {
-                put_k(buf + (i + 1 - first & 1) * Shape::TILE);
-                put_v(i + 1, buf + (i + 1 - first & 1) * Shape::TILE + TK * KS);
-            }
+            put_k(buf + (i + 1 - first & 1) * Shape::TILE);
+            put_v(i + 1, buf + (i + 1 - first & 1) * Shape::TILE + TK * KS);
         }
     } else {
         buf += kw * Shape::TILE;
         Place at = look_up(first + kw);
-        fetch_k(first + kw, at);
-        fetch_v(first + kw, at);
+        fetch(first + kw, at);
         at = look_up(first + kw + KW);
         for (u32 i = first + kw; i < last; i += KW) {
             put_k(buf);
@@ -507,8 +508,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             if (i + KW < last) {
-                fetch_k(i + KW, at);
-                fetch_v(i + KW, at);
+                fetch(i + KW, at);
                 at = look_up(i + 2 * KW);
             }
             work(i, buf);
@@ -524,12 +524,13 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll 1
         for (u32 i = RW > 1 ? first : first + kw; i < last; i += KW) {
             if (!partial(i)) continue;
-            const Place at = look_up(i);
 #pragma unroll 1
             for (int key = 0; key < TK; ++key) {
-                const int pg = __builtin_amdgcn_readlane(at.page, key), j = (int)((r.tile0 + i) * TK) + key;
-                if ((u32)pg >= a.n_pages) continue;
-                const T *v = vp + pg * a.vs[0] + (u32)__builtin_amdgcn_readlane(at.row, key) * a.vs[2];
+                const int j = (int)((r.tile0 + i) * TK) + key;
+                if (j >= r.kv) break;
+                const u32 pg = (u32)table[(u32)j / a.page_size];
+                if (pg >= a.n_pages) continue;
+                const T *v = vp + (i64)pg * a.vs[0] + (i64)((u32)j % a.page_size) * a.vs[2];
 #pragma unroll 1
                 for (u32 e0 = 0; e0 < a.head_dim; e0 += 64) {
                     const float x = e0 + lane < a.head_dim ? (float)v[e0 + lane] : 0.0f;
@@ -851,13 +852,23 @@ int ckks_clear_attend(const ckks_clear_attend_t *p, void *stream) {
     for (int i = 0; i < 2; ++i) a.qs[i] = p->q_stride[i], a.os[i] = p->out_stride[i];
     for (int i = 0; i < 3; ++i) a.ks[i] = g.k_stride[i], a.vs[i] = g.v_stride[i];
     a.ts = b.table_stride, a.q_start = b.d_q_start, a.kv_len = b.d_kv_len, a.table = b.d_page_table;
+    if (!g.n_pages) {  // nothing is a page: what is fetched in its place, and not used, comes from the queries
+        a.k = a.v = p->d_q;
+        for (int i = 0; i < 3; ++i) a.ks[i] = a.vs[i] = 0;
+    }
     a.n_seq = b.n_seq, a.n_tokens = b.n_tokens, a.n_pages = g.n_pages, a.page_size = g.page_size, a.table_width = b.table_width;
     a.kv_heads = g.kv_heads, a.heads = p->heads, a.group = p->heads / g.kv_heads, a.head_dim = g.head_dim;
     // a window of all positions is none
     a.window = p->window < (u64)b.table_width * g.page_size ? (int)p->window : 0, a.causal = p->flags & CKKS_CLEAR_CAUSAL;
-    a.page_shift = (g.page_size & (g.page_size - 1)) ? -1 : 31 - __builtin_clz(g.page_size);
-    const auto near = [&](i64 stride) { return stride >= 0 && stride < 1 << 24 && (u64)stride * g.page_size < 1u << 31; };
-    a.whole_rows = g.page_size % 16 == 0 && near(g.k_stride[2]) && near(g.v_stride[2]);
+    // positions are below 2^31: with l = ceil(log2(page_size)) the quotient by m = ceil(2^(31+l) / page_size) is exact
+    u32 l = 0;
+    while (l < 31 && (1u << l) < g.page_size) ++l;
+    const bool pow2 = (1u << l) == g.page_size;
+    a.page_mul = pow2 ? 0 : (u32)((((u64)1 << (31 + l)) + g.page_size - 1) / g.page_size);
+    a.page_shift = pow2 ? l : l - 1;
+    const auto near = [&](const i64 *st) { return st[0] >= 0 && st[0] < 1ll << 32 && st[2] >= 0 && st[2] < 1ll << 31 && (u64)st[2] * g.page_size < 1u << 31; };
+    a.near = near(a.ks) && near(a.vs);
+    a.alike = a.ks[0] == a.vs[0] && a.ks[2] == a.vs[2];
     a.tiles = n.tiles, a.splits = n.splits, a.min_tiles = n.min_tiles;
     a.c = p->scale * 1.44269504088896340736f;
     hipStream_t st = (hipStream_t)stream;

@@ -64,7 +64,7 @@ int ckks_clear_layer_norm_grad(const ckks_clear_norm_grad_t *a, void *stream);
 
 /* ---- key / value cache ---------------------------------------------------
  * Pages: d_k and d_v [n_pages][kv_heads][page_size][head_dim] by their strides {page, head, token}; head_dim a multiple
- * of 8, at most 256; any page_size >= 1.
+ * of 8, at most 256; any page_size >= 1.  A page stride is below 2^32 entries, the tokens of a page within 2^31.
  * Batch: n_seq sequences whose new tokens lie one after the other in n_tokens rows, sequence b in rows
  * q_start[b] .. q_start[b+1]-1 (int32 [n_seq+1], rising from 0 to n_tokens; values outside are clamped).  kv_len[b] counts the
  * tokens of sequence b with its new ones: new token i of n sits at position kv_len[b] - n + i.  Position p is row p % page_size

@@ -33,8 +33,8 @@ struct AttendArgs {
     const int32_t *q_start, *kv_len, *table;
     u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, group, head_dim, causal;
     int window;
-    u32 page_mul, page_shift;  // position / page_size = (position * page_mul >> 32) >> page_shift; page_mul 0: a shift alone
-    u32 near, alike;           // strides of pages and offsets within one fit 32 bits; keys and values have the same strides
+    u32 page_mul, page_shift;  // position / page_size = (2 * position * page_mul >> 32) >> page_shift
+    u32 alike;                 // keys and values have the same strides
     u32 tiles, splits, min_tiles;
     float c;             // scale * log2(e)
 };
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const u32 j = min((r.tile0 + tile) * TK + p * PASS + fetch_row, (u32)r.kv - 1);
-            const u32 n = a.page_mul ? __umulhi(j, a.page_mul) >> a.page_shift : j >> a.page_shift;
+            const u32 n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
             at.page[p] = (u32)table[n];
             at.row[p] = j - n * a.page_size;
         }
@@ -283,13 +283,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
                 s.none |= 1u << p;
             }
             if (ends && (r.tile0 + tile) * TK + p * PASS + fetch_row >= (u32)r.kv) s.none |= 1u << p;
-            if (a.near) {
-                s.k[p] = (u64)pg * (u32)a.ks[0] + (at.row[p] * (u32)a.ks[2] + lane_piece);
-                s.v[p] = a.alike ? s.k[p] : (u64)pg * (u32)a.vs[0] + (at.row[p] * (u32)a.vs[2] + lane_piece);
-            } else {
-                s.k[p] = (u64)pg * a.ks[0] + (u64)at.row[p] * a.ks[2] + lane_piece;
-                s.v[p] = (u64)pg * a.vs[0] + (u64)at.row[p] * a.vs[2] + lane_piece;
-            }
+            // check_cache: a page's stride fits 32 bits, and so does every offset within a page
+            s.k[p] = (u64)pg * (u32)a.ks[0] + (at.row[p] * (u32)a.ks[2] + lane_piece);
+            s.v[p] = a.alike ? s.k[p] : (u64)pg * (u32)a.vs[0] + (at.row[p] * (u32)a.vs[2] + lane_piece);
         }
         return s;
     };
@@ -368,6 +364,13 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
             for (int u = 0; u < SUB; ++u) s[u] = mma(row_frag(kb + (u * 32 + (lane & 31)) * KS + d * 16 + half * 8), qf[d], s[u]);
     };
     auto soften = [&](u32 tile) {
+        if (!seen(tile)) {
+#pragma unroll
+            for (int k = 0; k < 2 * SUB; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[k][j] = (T)0.0f;
+            return;
+        }
         if (masked(tile)) {
             const int from = see_lo(tile), to = see_hi(tile);
 #pragma unroll
@@ -452,31 +455,57 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         Sources next = locate(first + 1, at);
         fetch_k(next);
         at = look_up(first + 2);
-        // Past the last tile this moves what nobody reads.
-        auto stage = [&](u32 i) {
+        // Past the last tile these move what nobody reads.
+        auto put = [&](u32 i) {
             put_k(kb + (i + 1 & 1) * TK * KS);
             put_v(first + i, vb + (i & 1) * TK * VS);
+        };
+        auto move = [&](u32 i) {
             const Sources after = locate(first + i + 2, at);
             at = look_up(first + i + 3);
             fetch_v(next);
             fetch_k(after);
             next = after;
         };
+        // the first sum has weights 0 and no values yet
+        for (u32 x = threadIdx.x; x < TK * VS / E; x += 64 * RW) *(piece_t *)(vb + TK * VS + x * E) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < 2 * SUB; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[k][j] = (T)0.0f;
+        // The order of the products and the LDS reads that feed them: AHEAD fragments are under way before the first product,
+        // and one more (keys: one read, values: two) follows each product.
+        auto interleave = [] {
+            constexpr int MFMA = 0x8, READ = 0x100, AHEAD = 6, NK = SUB * DP / 16, NV = 2 * SUB * DT;
+            __builtin_amdgcn_sched_group_barrier(READ, AHEAD, 0);
+#pragma unroll
+            for (int x = 0; x < NK - AHEAD; ++x) {
+                __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(READ, 1, 0);
+            }
+#pragma unroll
+            for (int x = 0; x < NV; ++x) {
+                __builtin_amdgcn_sched_group_barrier(MFMA, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(READ, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(MFMA, AHEAD, 0);
+        };
         half_done();
         if (set) {
-            stage(0);
+            put(0);
+            move(0);
             half_done();
         }
         for (u32 i = 0; i <= n; ++i) {
             __builtin_amdgcn_s_setprio(1);
-            const bool now = i < n && seen(first + i), before = i && seen(first + i - 1);
-            const T *ki = kb + (i & 1) * TK * KS, *vi = vb + (i + 1 & 1) * TK * VS;
-            if (now) score(ki);
-            if (before) gather(vi);
+            if (i) move(i + set - 1);
+            score(kb + (i & 1) * TK * KS);
+            gather(vb + (i + 1 & 1) * TK * VS);
+            interleave();
             __builtin_amdgcn_s_setprio(0);
             half_done();
-            if (now) soften(first + i);
-            stage(i + set);
+            if (i < n) soften(first + i);
+            put(i + set);
             half_done();
         }
         if (!set) half_done();
@@ -860,14 +889,9 @@ int ckks_clear_attend(const ckks_clear_attend_t *p, void *stream) {
     a.kv_heads = g.kv_heads, a.heads = p->heads, a.group = p->heads / g.kv_heads, a.head_dim = g.head_dim;
     // a window of all positions is none
     a.window = p->window < (u64)b.table_width * g.page_size ? (int)p->window : 0, a.causal = p->flags & CKKS_CLEAR_CAUSAL;
-    // positions are below 2^31: with l = ceil(log2(page_size)) the quotient by m = ceil(2^(31+l) / page_size) is exact
-    u32 l = 0;
-    while (l < 31 && (1u << l) < g.page_size) ++l;
-    const bool pow2 = (1u << l) == g.page_size;
-    a.page_mul = pow2 ? 0 : (u32)((((u64)1 << (31 + l)) + g.page_size - 1) / g.page_size);
-    a.page_shift = pow2 ? l : l - 1;
-    const auto near = [&](const i64 *st) { return st[0] >= 0 && st[0] < 1ll << 32 && st[2] >= 0 && st[2] < 1ll << 31 && (u64)st[2] * g.page_size < 1u << 31; };
-    a.near = near(a.ks) && near(a.vs);
+    // positions are below 2^31: with l = ceil(log2(page_size)) the quotient by ceil(2^(31+l) / page_size) / 2^(31+l) is exact
+    while (a.page_shift < 31 && (1u << a.page_shift) < g.page_size) ++a.page_shift;
+    a.page_mul = (u32)((((u64)1 << (31 + a.page_shift)) + g.page_size - 1) / g.page_size);
     a.alike = a.ks[0] == a.vs[0] && a.ks[2] == a.vs[2];
     a.tiles = n.tiles, a.splits = n.splits, a.min_tiles = n.min_tiles;
     a.c = p->scale * 1.44269504088896340736f;

@@ -76,6 +76,11 @@ inline int check_cache(const char *who, const ckks_clear_pages_t &g, const ckks_
         set_error("%s: pages of type %u, %u rows, %u heads of %u entries", who, g.dtype, g.page_size, g.kv_heads, g.head_dim);
         return CKKS_E_INVAL;
     }
+    const auto near = [&](const i64 *st) { return st[0] >= 0 && st[0] < 1ll << 32 && st[1] >= 0 && st[2] >= 0 && st[2] < 1ll << 31 && (u64)st[2] * g.page_size < 1u << 31; };
+    if (!near(g.k_stride) || !near(g.v_stride)) {
+        set_error("%s: strides of the pages (a page's below 2^32 entries, a page itself below 2^31)", who);
+        return CKKS_E_INVAL;
+    }
     if (b.n_tokens >= 1u << 31 || b.n_seq >= 1u << 31 || (u64)b.table_width * g.page_size >= 1u << 31) {
         set_error("%s: %u tokens, %u sequences of up to %u pages of %u", who, b.n_tokens, b.n_seq, b.table_width, g.page_size);
         return CKKS_E_INVAL;

@@ -1,13 +1,16 @@
-// Rules on logits: history penalties, biases, mask.  A block takes a stretch of one row's vocabulary, tallies in LDS what the
-// row's history and bias list say about the tokens of that stretch, and then streams the logits through it once.  The tallies
-// are whole numbers (counts, and the largest list index of a bias), so their order cannot show in a result.
+// Rules on logits: history penalties, biases, mask.  A block takes a stretch of one row's vocabulary.  It tallies in LDS what the
+// row's history and bias list say about the tokens of that stretch, works out the few logits that they change, streams the stretch
+// through the mask, and then writes the changed ones over it: the many logits cost no more than a masked copy.  The tallies are
+// whole numbers, and of several biases the largest index counts: no order shows in a result.
 #include <algorithm>
 
 #include "clear_device.h"
 
 namespace ckks {
 
-constexpr u32 SEEN = 1u << 31;  // tally: in the prompt; the bits below count the generated ones
+// Tally of a token: it is in the prompt; the row's bias list has it; below these how often it was generated.
+constexpr u32 SEEN = 1u << 31, BIASED = 1u << 30, COUNT = BIASED - 1;
+constexpr u32 LISTED = 1024;  // biases of a stretch that are kept in LDS
 
 struct LogitsArgs {
     const void *logits;
@@ -23,100 +26,164 @@ struct LogitsArgs {
 
 __device__ __forceinline__ u32 clamp_at(int32_t v, u32 top) { return v < 0 ? 0u : min((u32)v, top); }
 
-// THREADS x V x R entries per block.
-template <class T, class TO, int THREADS, int R, bool HISTORY, bool BIAS>
+// Up to four ids, zeros behind the last.
+__device__ __forceinline__ Pack<int32_t, 4> load_ids(const int32_t *p, u32 n) {
+    if (n >= 4) return load_pack<4>(p);
+    Pack<int32_t, 4> t{};
+    for (u32 k = 0; k < n; ++k) t.v[k] = p[k];
+    return t;
+}
+
+// use(token - first, index) for the thread's part of the history, ids within the stretch only; `t` holds its first four.
+template <class F>
+__device__ __forceinline__ void each_token(const LogitsArgs &a, u32 h0, u32 h1, Pack<int32_t, 4> t, u32 threads, u32 first, u32 span, F use) {
+    for (u32 i = h0 + 4 * threadIdx.x; i < h1;) {
+#pragma unroll
+        for (u32 k = 0; k < 4; ++k) {
+            const u32 c = (u32)t.v[k] - first;
+            if (i + k < h1 && c < span) use(c, i + k);
+        }
+        i += 4 * threads;
+        if (i < h1) t = load_ids(a.tokens + i, h1 - i);
+    }
+}
+
+// Of the biases for token `c` of the stretch the one with the largest index: from LDS where the stretch's biases fit there.
+__device__ __forceinline__ float last_bias(const LogitsArgs &a, u32 c, u32 first, u32 b0, u32 b1, const u32 (*listed)[2], u32 n) {
+    u32 best = b0;
+    if (n <= LISTED) {
+        for (u32 k = 0; k < n; ++k)
+            if (listed[k][0] == c) best = max(best, listed[k][1]);
+    } else {
+        for (u32 b = b1; b-- > b0;)
+            if ((u32)a.bias_ids[b] - first == c) {
+                best = b;
+                break;
+            }
+    }
+    return a.bias[best];
+}
+
+// THREADS x V x R entries per block.  RULES: there is a history or a bias list.
+template <class T, class TO, int THREADS, int R, bool RULES>
 __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
     constexpr int V = 8, SPAN = THREADS * V * R;
-    __shared__ __attribute__((aligned(16))) u32 tally[HISTORY ? SPAN : 4];
-    __shared__ __attribute__((aligned(16))) u32 which[BIAS ? SPAN : 4];
+    __shared__ __attribute__((aligned(16))) u32 tally[RULES ? SPAN : 4];   // then the changed logits
+    __shared__ u32 taken[RULES ? SPAN / 32 : 1];                           // a bit for each token that somebody works out
+    __shared__ u32 listed[RULES ? LISTED : 1][2], n_listed;                // {token, index in the bias list}
     const u32 row = blockIdx.x / a.tiles, first = (blockIdx.x % a.tiles) * SPAN, span = min(a.vocab - first, (u32)SPAN);
     const T *in = (const T *)a.logits + (i64)row * a.ls + first;
     TO *out = (TO *)a.out + (i64)row * a.os + first;
+    const int32_t *mask = a.mask ? a.mask + (i64)row * a.ms : nullptr;
+    // the stretch is under way while the rules are worked out
     Pack<T, V> x[R];
+    u32 bits[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const u32 c = (r * THREADS + threadIdx.x) * V;
         x[r] = load_part<V>(in + c, c < span ? (int)min(span - c, (u32)V) : 0);
+        // `first` and c are multiples of 8: a thread's eight bits lie in one byte of the mask
+        bits[r] = mask && c < span ? (u32)mask[(first + c) >> 5] >> ((first + c) & 31) : 0xffu;
     }
-    if (HISTORY || BIAS) {
-        if (HISTORY)
-            for (u32 i = threadIdx.x; i < SPAN / 4; i += THREADS) ((uint4 *)tally)[i] = make_uint4(0, 0, 0, 0);
-        if (BIAS)
-            for (u32 i = threadIdx.x; i < SPAN / 4; i += THREADS) ((uint4 *)which)[i] = make_uint4(0, 0, 0, 0);
+    u32 h0 = 0, h1 = 0, b0 = 0, b1 = 0;
+    Pack<int32_t, 4> t0{};
+    if (RULES) {
+        u32 made = 0;
+        if (a.tokens) {
+            h0 = clamp_at(a.token_start[row], a.n_tokens);
+            h1 = clamp_at(a.token_start[row + 1], a.n_tokens);
+            made = a.n_prompt ? h0 + clamp_at(a.n_prompt[row], a.n_tokens) : h0;
+        }
+        if (a.bias) {
+            b0 = clamp_at(a.bias_start[row], a.n_biases);
+            b1 = clamp_at(a.bias_start[row + 1], a.n_biases);
+        }
+        const u32 i0 = h0 + 4 * threadIdx.x;
+        if (i0 < h1) t0 = load_ids(a.tokens + i0, h1 - i0);
+        const float rep = a.repetition ? a.repetition[row] : 1.0f, freq = a.frequency ? a.frequency[row] : 0.0f,
+                    pres = a.presence ? a.presence[row] : 0.0f;
+        for (u32 k = threadIdx.x; k < SPAN / 4; k += THREADS) ((uint4 *)tally)[k] = make_uint4(0, 0, 0, 0);
+        for (u32 k = threadIdx.x; k < SPAN / 32; k += THREADS) taken[k] = 0;
+        if (threadIdx.x == 0) n_listed = 0;
         __syncthreads();
-        if (HISTORY) {
-            const u32 h0 = clamp_at(a.token_start[row], a.n_tokens), h1 = clamp_at(a.token_start[row + 1], a.n_tokens);
-            const u32 made = a.n_prompt ? h0 + clamp_at(a.n_prompt[row], a.n_tokens) : h0;
-            for (u32 i = h0 + threadIdx.x; i < h1; i += THREADS) {
-                const u32 c = (u32)a.tokens[i] - first;
-                if (c < span) {
-                    if (i < made)
-                        atomicOr(&tally[c], SEEN);
-                    else
-                        atomicAdd(&tally[c], 1u);
-                }
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32 i) {
+            if (i < made)
+                atomicOr(&tally[c], SEEN);
+            else
+                atomicAdd(&tally[c], 1u);
+        });
+        for (u32 b = b0 + threadIdx.x; b < b1; b += THREADS) {
+            const u32 c = (u32)a.bias_ids[b] - first;
+            if (c >= span) continue;
+            atomicOr(&tally[c], BIASED);
+            const u32 at = atomicAdd(&n_listed, 1u);
+            if (at < LISTED) {
+                listed[at][0] = c;
+                listed[at][1] = b;
             }
         }
-        if (BIAS) {
-            const u32 b0 = clamp_at(a.bias_start[row], a.n_biases), b1 = clamp_at(a.bias_start[row + 1], a.n_biases);
-            for (u32 i = b0 + threadIdx.x; i < b1; i += THREADS) {
-                const u32 c = (u32)a.bias_ids[i] - first;
-                if (c < span) atomicMax(&which[c], i + 1);
-            }
-        }
         __syncthreads();
+        // whoever comes first to a token works it out, and leaves the result in place of the tally
+        auto change = [&](u32 c) {
+            if (atomicOr(&taken[c >> 5], 1u << (c & 31)) >> (c & 31) & 1) return;
+            const u32 t = tally[c], n = t & COUNT;
+            float l = (float)in[c];
+            if (t & ~BIASED) l = l > 0.0f ? l / rep : l * rep;
+            l = l - freq * (float)n;
+            l = l - (n ? pres : 0.0f);
+            if (t & BIASED) l += last_bias(a, c, first, b0, b1, listed, n_listed);
+            if (mask && !((u32)mask[(first + c) >> 5] >> ((first + c) & 31) & 1)) l = -__builtin_inff();
+            tally[c] = __float_as_uint(l);
+        };
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32) { change(c); });
+        for (u32 b = b0 + threadIdx.x; b < b1; b += THREADS) {
+            const u32 c = (u32)a.bias_ids[b] - first;
+            if (c < span) change(c);
+        }
+        __syncthreads();  // d_out may be d_logits: all that is changed has been read
     }
-    const float rep = HISTORY && a.repetition ? a.repetition[row] : 1.0f, freq = HISTORY && a.frequency ? a.frequency[row] : 0.0f,
-                pres = HISTORY && a.presence ? a.presence[row] : 0.0f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const u32 c = (r * THREADS + threadIdx.x) * V;
         if (c >= span) break;
-        // `first` and c are multiples of 8: a thread's eight bits lie in one byte of the mask
-        const u32 bits = a.mask ? (u32)a.mask[(i64)row * a.ms + ((first + c) >> 5)] >> ((first + c) & 31) : 0xffu;
         Pack<TO, V> y;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            float l = (float)x[r].v[i];
-            if (HISTORY) {
-                const u32 t = tally[c + i], n = t & (SEEN - 1);
-                if (t) {
-                    l = l > 0.0f ? l / rep : l * rep;
-                    l = l - freq * (float)n;
-                    l = l - (n ? pres : 0.0f);
-                }
-            }
-            if (BIAS) {
-                const u32 b = which[c + i];
-                if (b) l += a.bias[b - 1];
-            }
-            y.v[i] = (TO)((bits >> i) & 1 ? l : -__builtin_inff());
-        }
+        for (int i = 0; i < V; ++i) y.v[i] = (TO)((bits[r] >> i) & 1 ? (float)x[r].v[i] : -__builtin_inff());
         store_part<V>(out + c, y, (int)min(span - c, (u32)V));
+    }
+    if (RULES) {
+        __threadfence_block();
+        __syncthreads();  // the stretch is written: now the changed logits
+        auto write = [&](u32 c) {
+            if (atomicAnd(&taken[c >> 5], ~(1u << (c & 31))) >> (c & 31) & 1) out[c] = (TO)__uint_as_float(tally[c]);
+        };
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32) { write(c); });
+        for (u32 b = b0 + threadIdx.x; b < b1; b += THREADS) {
+            const u32 c = (u32)a.bias_ids[b] - first;
+            if (c < span) write(c);
+        }
     }
 }
 
 template <class T, class TO>
 static void launch_logits(LogitsArgs a, u32 rows, hipStream_t st) {
-    const bool h = a.tokens, b = a.bias;
-    // 8192 entries a block: each block reads the row's whole history, so a long stretch reads it less often; 2048 where that
-    // leaves most of the 256 CUs without a block
-    const bool small = (u64)rows * ((a.vocab + 8191) / 8192) < 256;
-    const u32 span = small ? 2048 : 8192;
+    // 16384 entries a block: each block goes through the row's whole history, so long stretches go through it less often; 2048
+    // where that leaves most of the 256 CUs without a block
+    const bool small = (u64)rows * ((a.vocab + 16383) / 16384) < 256;
+    const u32 span = small ? 2048 : 16384;
     a.tiles = (a.vocab + span - 1) / span;
     const dim3 grid(rows * a.tiles);
-#define CKKS_LOGITS(H, B)                                                                                          \
-    if (h == H && b == B) {                                                                                        \
-        if (small)                                                                                                 \
-            hipLaunchKernelGGL((logits_kernel<T, TO, 256, 1, H, B>), grid, dim3(256), 0, st, a);                   \
-        else                                                                                                       \
-            hipLaunchKernelGGL((logits_kernel<T, TO, 512, 2, H, B>), grid, dim3(512), 0, st, a);                   \
+    if (a.tokens || a.bias) {
+        if (small)
+            hipLaunchKernelGGL((logits_kernel<T, TO, 256, 1, true>), grid, dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((logits_kernel<T, TO, 1024, 2, true>), grid, dim3(1024), 0, st, a);
+    } else {
+        if (small)
+            hipLaunchKernelGGL((logits_kernel<T, TO, 256, 1, false>), grid, dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((logits_kernel<T, TO, 1024, 2, false>), grid, dim3(1024), 0, st, a);
     }
-    CKKS_LOGITS(false, false)
-    CKKS_LOGITS(false, true)
-    CKKS_LOGITS(true, false)
-    CKKS_LOGITS(true, true)
-#undef CKKS_LOGITS
 }
 
 }  // namespace ckks
@@ -141,7 +208,7 @@ extern "C" int ckks_clear_logits(const ckks_clear_logits_t *p, void *stream) {
         set_error("ckks_clear_logits: tokens and penalties need d_token_start, biases d_bias_start");
         return CKKS_E_INVAL;
     }
-    if (p->n_tokens >= 1u << 31 || p->n_biases >= 1u << 31 || p->vocab >= 1u << 31 || (u64)p->rows * ((p->vocab + 2047) / 2048) >= 1u << 31) {
+    if (p->n_tokens >= 1u << 30 || p->n_biases >= 1u << 30 || p->vocab >= 1u << 31 || (u64)p->rows * ((p->vocab + 2047) / 2048) >= 1u << 31) {
         set_error("ckks_clear_logits: %u rows of %u, %u tokens, %u biases exceed one launch", p->rows, p->vocab, p->n_tokens, p->n_biases);
         return CKKS_E_INVAL;
     }

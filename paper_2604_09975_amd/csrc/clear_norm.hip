@@ -2,6 +2,7 @@
 // bound by memory.  The weight's and bias's gradients are column sums: each group keeps them for the columns that it holds
 // over all its rows, writes them once, and a second kernel adds the groups' sums in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "clear_device.h"
 
@@ -40,21 +41,46 @@ __device__ __forceinline__ void group_sum2(float &p, float &q, float (*ex)[2][2]
     }
 }
 
-// E entries of a row per thread, in chunks of 16 bytes that lie TPR chunks apart.
+// A thread's E entries of a row: chunks of 16 bytes, TPR chunks apart.  A chunk that would pass the end of the row is moved back
+// to end with it, and its first `skip` entries belong to others (all of it: the thread has no such chunk).  So every load is one
+// of full width without a branch around it -- a branch would have the result waited for at once -- and what is stored twice is
+// stored with the same bits.  Rows have at least one chunk.
+template <int V, int K, int TPR>
+struct Columns {
+    u32 col[K];
+    int skip[K];
+    bool ragged;  // some thread skips something
+    __device__ __forceinline__ Columns(u32 cols, u32 t) {
+        ragged = cols != (u32)(V * K * TPR);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const u32 c = (k * TPR + t) * V;
+            col[k] = min(c, cols - V);
+            skip[k] = (int)min(c - col[k], (u32)V);
+        }
+    }
+};
+
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
     __shared__ float ex[TPR / 64][2][2];
     u32 slot = 0;
     const u32 t = threadIdx.x % TPR, groups = gridDim.x * (THREADS / TPR);
-    int n[K];
+    const Columns<V, K, TPR> at(a.cols, t);
+    u32 row = blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR;
+    Pack<T, V> next[K];
+    auto fetch = [&](u32 r) {
+        const T *x = (const T *)a.x + (i64)min(r, a.rows - 1) * a.xs;
+#pragma unroll
+        for (int k = 0; k < K; ++k) next[k] = load_pack<V>(x + at.col[k]);
+    };
+    fetch(row);
     float w[K][V], b[K][V];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const u32 col = (k * TPR + t) * V;
-        n[k] = col < a.cols ? (int)min(a.cols - col, (u32)V) : 0;
-        const Pack<TW, V> pw = a.w ? load_part<V>((const TW *)a.w + col, n[k]) : Pack<TW, V>{};
-        const Pack<TW, V> pb = a.b ? load_part<V>((const TW *)a.b + col, n[k]) : Pack<TW, V>{};
+        const Pack<TW, V> pw = a.w ? load_pack<V>((const TW *)a.w + at.col[k]) : Pack<TW, V>{};
+        const Pack<TW, V> pb = a.b ? load_pack<V>((const TW *)a.b + at.col[k]) : Pack<TW, V>{};
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             w[k][i] = a.w ? (float)pw.v[i] : 1.0f;
@@ -62,18 +88,23 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
         }
     }
     const float inv = 1.0f / (float)a.cols;
-    for (u32 row = blockIdx.x * (THREADS / TPR) + threadIdx.x / TPR; row < a.rows; row += groups) {
-        const T *x = (const T *)a.x + (i64)row * a.xs;
-        T *y = (T *)a.y + (i64)row * a.ys;
+    for (; row < a.rows; row += groups) {
         float v[K][V], s = 0.0f, none = 0.0f;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const Pack<T, V> p = load_part<V>(x + (k * TPR + t) * V, n[k]);
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                v[k][i] = (float)p.v[i];
-                s += v[k][i];
-            }
+            for (int i = 0; i < V; ++i) v[k][i] = (float)next[k].v[i];
+        fetch(row + groups);  // the next row is under way while this one is worked on
+        if (at.ragged) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s += i >= at.skip[k] ? v[k][i] : 0.0f;
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) s += v[k][i];
         }
         group_sum2<TPR>(s, none, ex, slot);
         const float mean = s * inv;
@@ -81,11 +112,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = i < n[k] ? v[k][i] - mean : 0.0f;
-                v[k][i] = d;
-                q = __builtin_fmaf(d, d, q);
-            }
+            for (int i = 0; i < V; ++i) v[k][i] -= mean;
+        if (at.ragged) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) q = __builtin_fmaf(i >= at.skip[k] ? v[k][i] : 0.0f, v[k][i], q);
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) q = __builtin_fmaf(v[k][i], v[k][i], q);
+        }
         none = 0.0f;
         group_sum2<TPR>(q, none, ex, slot);
         const float r = 1.0f / sqrtf(__builtin_fmaf(q, inv, a.eps));
@@ -93,59 +131,80 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
             a.mean[row] = mean;
             a.rstd[row] = r;
         }
+        T *y = (T *)a.y + (i64)row * a.ys;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             Pack<T, V> p;
 #pragma unroll
             for (int i = 0; i < V; ++i) p.v[i] = (T)__builtin_fmaf(v[k][i] * r, w[k][i], b[k][i]);
-            store_part<V>(y + (k * TPR + t) * V, p, n[k]);
+            if (at.skip[k] < V) store_pack<V>(y + at.col[k], p);
         }
     }
 }
 
+// The weight lies in LDS: registers hold the sums of the columns and the row that comes next.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR, GROUPS = THREADS / TPR;
     __shared__ float ex[TPR / 64][2][2];
+    __shared__ __attribute__((aligned(16))) float weight[K][TPR][V];
     u32 slot = 0;
     const u32 t = threadIdx.x % TPR, groups = gridDim.x * GROUPS;
-    int n[K];
-    float w[K][V], dw[K][V], db[K][V];
+    const Columns<V, K, TPR> at(a.cols, t);
+    u32 row = blockIdx.x * GROUPS + threadIdx.x / TPR;
+    Pack<T, V> next_x[K], next_d[K];
+    float next_mean, next_r;
+    auto fetch = [&](u32 r) {
+        r = min(r, a.rows - 1);
+        const T *x = (const T *)a.x + (i64)r * a.xs, *dy = (const T *)a.dy + (i64)r * a.dys;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            next_x[k] = load_pack<V>(x + at.col[k]);
+            next_d[k] = load_pack<V>(dy + at.col[k]);
+        }
+        next_mean = a.mean[r];
+        next_r = a.rstd[r];
+    };
+    fetch(row);
+    float dw[K][V], db[K][V];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const u32 col = (k * TPR + t) * V;
-        n[k] = col < a.cols ? (int)min(a.cols - col, (u32)V) : 0;
-        const Pack<TW, V> pw = a.w ? load_part<V>((const TW *)a.w + col, n[k]) : Pack<TW, V>{};
+        const Pack<TW, V> pw = a.w ? load_pack<V>((const TW *)a.w + at.col[k]) : Pack<TW, V>{};
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            w[k][i] = a.w ? (float)pw.v[i] : 1.0f;
+            if (threadIdx.x < TPR) weight[k][t][i] = a.w ? (float)pw.v[i] : 1.0f;
             dw[k][i] = db[k][i] = 0.0f;
         }
     }
+    __syncthreads();
     const float inv = 1.0f / (float)a.cols;
-    for (u32 row = blockIdx.x * GROUPS + threadIdx.x / TPR; row < a.rows; row += groups) {
-        const T *x = (const T *)a.x + (i64)row * a.xs, *dy = (const T *)a.dy + (i64)row * a.dys;
-        const float mean = a.mean[row], r = a.rstd[row];
-        float xh[K][V], g[K][V], s1 = 0.0f, s2 = 0.0f;
+    for (; row < a.rows; row += groups) {
         Pack<T, V> px[K], pd[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            px[k] = load_part<V>(x + (k * TPR + t) * V, n[k]);
-            pd[k] = load_part<V>(dy + (k * TPR + t) * V, n[k]);
+            px[k] = next_x[k];
+            pd[k] = next_d[k];
         }
-        // behind the row's end dy is 0, and so is everything that it meets
+        const float mean = next_mean, r = next_r;
+        fetch(row + groups);
+        float s1 = 0.0f, s2 = 0.0f;
+        auto sums = [&](auto ragged) {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float d = (float)pd[k].v[i], h = ((float)px[k].v[i] - mean) * r;
-                xh[k][i] = h;
-                g[k][i] = d * w[k][i];
-                dw[k][i] = __builtin_fmaf(d, h, dw[k][i]);
-                db[k][i] += d;
-                s1 += g[k][i];
-                s2 = __builtin_fmaf(g[k][i], h, s2);
-            }
+                for (int i = 0; i < V; ++i) {
+                    const float d = !ragged.value || i >= at.skip[k] ? (float)pd[k].v[i] : 0.0f, h = ((float)px[k].v[i] - mean) * r;
+                    const float g = d * weight[k][t][i];
+                    dw[k][i] = __builtin_fmaf(d, h, dw[k][i]);
+                    db[k][i] += d;
+                    s1 += g;
+                    s2 = __builtin_fmaf(g, h, s2);
+                }
+        };
+        if (at.ragged)
+            sums(std::true_type());
+        else
+            sums(std::false_type());
         if (!a.y) continue;
         group_sum2<TPR>(s1, s2, ex, slot);
         s1 *= inv;
@@ -155,8 +214,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormAr
         for (int k = 0; k < K; ++k) {
             Pack<T, V> p;
 #pragma unroll
-            for (int i = 0; i < V; ++i) p.v[i] = (T)(r * (g[k][i] - s1 - xh[k][i] * s2));
-            store_part<V>(dx + (k * TPR + t) * V, p, n[k]);
+            for (int i = 0; i < V; ++i)
+                p.v[i] = (T)(r * ((float)pd[k].v[i] * weight[k][t][i] - s1 - ((float)px[k].v[i] - mean) * r * s2));
+            if (at.skip[k] < V) store_pack<V>(dx + at.col[k], p);
         }
     }
     if (!a.part) return;
@@ -165,13 +225,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormAr
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const u32 col = (k * TPR + t) * V + i;
-                if (i < n[k]) {
-                    part[col] = dw[k][i];
-                    part[a.cols + col] = db[k][i];
+            for (int i = 0; i < V; ++i)
+                if (i >= at.skip[k]) {
+                    part[at.col[k] + i] = dw[k][i];
+                    part[a.cols + at.col[k] + i] = db[k][i];
                 }
-            }
         return;
     }
     // the block's groups hold the same columns: joined here, a quarter as many sums reach memory
@@ -187,11 +245,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormAr
         }
         __syncthreads();
         for (u32 c = threadIdx.x; c < 2 * TPR * V; c += THREADS) {
-            const u32 which = c / (TPR * V), col = c % (TPR * V);
+            const u32 which = c / (TPR * V), j = c % (TPR * V), begin = (k * TPR + j / V) * V, col = min(begin, a.cols - V) + j % V;
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < GROUPS; ++i) s += join[i][which][col];
-            if ((u32)k * TPR * V + col < a.cols) part[which * (size_t)a.cols + k * TPR * V + col] = s;
+            for (int i = 0; i < GROUPS; ++i) s += join[i][which][j];
+            if (col >= begin) part[which * (size_t)a.cols + col] = s;
         }
     }
 }
@@ -290,29 +348,32 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restric
 }
 
 // Threads per row and entries per thread: the smallest group whose registers hold the row at up to 32 entries a thread
-// (16 where 1024 threads share the register file).  0: none does.
+// (16 where 1024 threads share the register file).  0: none does, or the row is shorter than an access.
 struct NormShape {
     u32 tpr, e;
 };
 static NormShape norm_shape(u32 cols) {
+    if (cols < 8) return {0, 0};
     if (cols <= 64 * 32) return {64, cols <= 64 * 8 ? 8u : cols <= 64 * 16 ? 16u : 32u};
     if (cols <= 256 * 32) return {256, cols <= 256 * 16 ? 16u : 32u};
     if (cols <= 1024 * 16) return {1024, 16};
     return {0, 0};
 }
-// Blocks of the gradient, each of which leaves one pair of column sums: two to four blocks for each of 256 CUs.
+// Blocks: as many as the registers let run at once on 256 CUs, each with every so-manieth row.  Each block of the gradient leaves
+// one pair of column sums.
+static u32 norm_blocks(u32 rows, const NormShape &s, bool grad) {
+    const u32 per = s.tpr == 64 ? 4 : 1, cu = s.tpr == 1024 ? 1 : grad ? (s.e == 32 ? 2 : s.e == 16 ? 4 : 6) : (s.e == 32 ? 3 : 6);
+    return std::min<u32>((rows + per - 1) / per, 256 * cu);
+}
 static u32 norm_grad_blocks(u32 rows, u32 cols) {
     const NormShape s = norm_shape(cols);
-    if (!s.tpr) return std::min<u32>(rows, 64);
-    const u32 per = s.tpr == 64 ? 4 : 1;
-    return std::min<u32>((rows + per - 1) / per, 512);
+    return s.tpr ? norm_blocks(rows, s, true) : std::min<u32>(rows, 64);
 }
 
 template <class T, class TW>
 static void launch_norm(const NormArgs &a, hipStream_t st) {
     const NormShape s = norm_shape(a.cols);
-    const u32 per = s.tpr == 64 ? 4 : 1;
-    const u32 blocks = std::min<u32>((a.rows + per - 1) / per, 2048);
+    const u32 blocks = s.tpr ? norm_blocks(a.rows, s, false) : 0;
 #define CKKS_NORM(TPR, E) \
     if (s.tpr == TPR && s.e == E) {                                                                                      \
         hipLaunchKernelGGL((norm_kernel<T, TW, TPR, E>), dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);         \

@@ -6,7 +6,7 @@
 // lane but for one exchange between the halves, and the weights come out in the order in which the next product,
 // O^T = V^T P^T, wants them.  Neither scores nor weights pass through LDS.
 //
-//   RW = 4: four waves of 32 rows share each tile of keys and values (chunks of a prompt).
+//   RW = 4, 8: waves of 32 rows share each tile of keys and values (chunks of a prompt).
 //   KW > 1: one set of 32 rows, each wave takes every KW-th tile through its own stretch of LDS, without barriers, and the
 //           waves' results are joined at the end (single tokens: the time is that of reading the cache).
 // Either may split the keys over several blocks; a second kernel then joins the blocks' results in order.
@@ -748,13 +748,30 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void attend_join_kern
 }
 
 // ---- host ----
+// The forms of the kernel and what they cost, measured on prompts and single tokens with many and with few blocks: a block does
+// `rows` rows, a step of `keys` keys takes step_us where it has its CU for itself and full_us where `fit` blocks share it, and
+// begin_us goes into finding its rows, its first keys and its output.
+struct AttendForm {
+    u32 waves_rows, rows, tk, keys;  // RW; rows of a block; keys of a tile and of a step
+    float begin_us, step_us, full_us;
+    u32 fit;
+};
+constexpr AttendForm FORMS_64[] = {{1, 32, 32, 128, 6, 1.1f, 1.6f, 2}, {4, 128, 64, 64, 7, 1.3f, 2.3f, 3}};
+constexpr AttendForm FORMS_128[] = {{1, 32, 32, 128, 6, 1.7f, 2.8f, 2}, {4, 128, 64, 64, 8, 1.8f, 2.6f, 2}, {8, 256, 64, 64, 10, 1.9f, 1.9f, 1}};
+constexpr AttendForm FORMS_256[] = {{1, 32, 32, 128, 8, 4, 4, 1}, {4, 128, 32, 32, 10, 2.2f, 2.2f, 1}};
+// 32-bit products are slow enough for the waves of a row tile to read their keys apart; rows of 256 do not fit so.
+constexpr AttendForm FORMS_F32_64[] = {{1, 32, 32, 128, 6, 4, 4, 1}};
+constexpr AttendForm FORMS_F32_128[] = {{1, 32, 32, 128, 6, 8, 8, 1}};
+constexpr AttendForm FORMS_F32_256[] = {{4, 128, 32, 32, 10, 14, 14, 1}};
+
 struct AttendPlan {
-    bool wide;          // four waves of 32 rows on shared tiles
+    AttendForm form;
     u32 dp, tiles, splits, min_tiles;
     u64 work_bytes;
 };
 
-// Which kernel and how many splits, from the sizes alone.
+// The form and the number of splits that the measured costs promise the least time for.  Lengths are on the device: the table's
+// width bounds them, and sequences are taken to be of equal shares of the new tokens.
 static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
     const ckks_clear_pages_t &g = p.pages;
     const ckks_clear_batch_t &b = p.batch;
@@ -762,25 +779,51 @@ static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
         p.heads > 1u << 16)
         return false;
     const u64 group = p.heads / g.kv_heads, rows = (u64)b.n_tokens * group, seqs = std::min(b.n_seq, b.n_tokens);
-    const u64 keys = (u64)b.table_width * g.page_size;
-    if (rows >= 1u << 31 || keys >= 1u << 31 || b.n_seq >= 1u << 31) return false;
+    const u64 width = (u64)b.table_width * g.page_size;
+    if (rows >= 1u << 31 || width >= 1u << 31 || b.n_seq >= 1u << 31) return false;
     n.dp = g.head_dim <= 64 ? 64 : g.head_dim <= 128 ? 128 : 256;
     const bool f32 = g.dtype == CKKS_CLEAR_F32;
-    // Sharing tiles reads keys and values a quarter as often; it needs enough row tiles of 128 to fill 256 CUs.
-    const u64 wide_rows = f32 || n.dp == 256 ? 128 : 256;
-    n.wide = rows / 128 * g.kv_heads >= 256 || (f32 && n.dp == 256);
-    const u64 r = n.wide ? wide_rows : 32;
-    const u64 tiles = rows / r + seqs;                       // at most
-    const u64 likely = seqs ? seqs * ((rows / seqs + r - 1) / r) : 0;
-    const u64 blocks = std::max<u64>(likely * g.kv_heads, 1);
-    const u32 tk = n.wide && !f32 && n.dp <= 128 ? 64 : 32;
-    // A split has 512 keys at least.  Eight blocks for each CU: sequences of different lengths then even out.
-    n.min_tiles = 512 / tk;
-    const u64 most = std::max<u64>(1, keys / 512);
-    const u64 want = n.wide ? (wide_rows == 256 ? 256 : 512) : 2048;
-    n.splits = (u32)std::min<u64>(most, blocks >= want ? 1 : (want + blocks - 1) / blocks);
+    const AttendForm *forms = f32 ? (n.dp == 64 ? FORMS_F32_64 : n.dp == 128 ? FORMS_F32_128 : FORMS_F32_256)
+                                  : (n.dp == 64 ? FORMS_64 : n.dp == 128 ? FORMS_128 : FORMS_256);
+    const u32 count = f32 ? 1 : n.dp == 128 ? 3 : 2;
+    constexpr double CUS = 256, READ = 4.9e6, JOIN = 1.5e6;  // bytes a microsecond
+    const double per_seq = seqs ? (double)rows / seqs : 0, causal = p.flags & CKKS_CLEAR_CAUSAL;
+    double keys = (double)width - (causal ? per_seq / group / 2 : 0);  // that a row sees, about
+    if (p.window && p.window < width) keys = std::min<double>(keys, p.window + per_seq / group);
+    keys = std::max(keys, 1.0);
+    const double key_bytes = 2.0 * g.head_dim * clear_dtype_bytes(g.dtype), all = seqs * g.kv_heads * keys * key_bytes;
+    double best = 0;
+    n.splits = 0;
+    for (u32 f = 0; f < count; ++f) {
+        const AttendForm &form = forms[f];
+        const double blocks = (seqs ? seqs * std::ceil(per_seq / form.rows) : 1) * g.kv_heads;
+        const double most = std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));
+        auto consider = [&](u32 splits) {
+            if (splits < 1 || splits > most) return;
+            const double load = blocks * splits / CUS, steps = std::ceil(keys / splits / form.keys);
+            const double share = form.fit > 1 ? std::min(1.0, std::max(0.0, (load - 1) / (form.fit - 1))) : 0.0;
+            const double step = form.step_us + share * (form.full_us - form.step_us), rounds = load / form.fit;
+            const double work = (rounds <= 1 ? 1 : rounds < 3 ? std::ceil(rounds) : rounds + 0.5) * (form.begin_us + steps * step);
+            // Reading the cache: slower with fewer CUs at it, or with one block on some and two on others; where sequences differ
+            // in length, part of a block is left at the end.
+            double read = all / READ / std::min(1.0, 1.3 * load);
+            if (load > 1) read *= 0.5 + 0.5 * std::ceil(load) / load;
+            if (seqs > 1) read += 0.15 * steps * form.keys * key_bytes * CUS * form.fit / READ;
+            const double join = splits > 1 ? 5 + (double)b.n_tokens * p.heads * g.head_dim * 8 * splits / JOIN : 0;
+            const double us = std::max(work, form.begin_us + read) + join;
+            if (!n.splits || us < best) {
+                best = us;
+                n.form = form;
+                n.splits = splits;
+            }
+        };
+        for (u32 splits = 1; splits <= most; splits += std::max(1u, splits / 2)) consider(splits);
+        for (u32 k = 1; k <= 2; ++k) consider((u32)std::min(1024.0, k * CUS / blocks));  // as many blocks as CUs, or twice that
+    }
+    const u64 tiles = rows / n.form.rows + seqs;  // at most
     if (tiles * g.kv_heads * n.splits >= 1u << 31) return false;
     n.tiles = (u32)tiles;
+    n.min_tiles = 4;
     n.work_bytes = n.splits > 1 ? (u64)n.splits * b.n_tokens * p.heads * (g.head_dim + 1) * 4 : 0;
     return true;
 }
@@ -804,16 +847,17 @@ static int launch_attend(const AttendArgs &a, hipStream_t st) {
 }
 template <class T>
 static int launch_attend(const AttendArgs &a, const AttendPlan &n, hipStream_t st) {
-    constexpr bool f32 = sizeof(T) == 4;
-    if (n.wide) {
-        if (n.dp == 64) return launch_attend<T, 64, f32 ? 4 : 8, 1, f32 ? 32 : 64, 2>(a, st);
-        if (n.dp == 128) return launch_attend<T, 128, f32 ? 4 : 8, 1, f32 ? 32 : 64, f32 ? 1 : 2>(a, st);
+    if constexpr (sizeof(T) == 4) {
+        if (n.dp == 64) return launch_attend<T, 64, 1, 4, 32, 1>(a, st);
+        if (n.dp == 128) return launch_attend<T, 128, 1, 4, 32, 1>(a, st);
         return launch_attend<T, 256, 4, 1, 32, 1>(a, st);
+    } else {
+        if (n.dp == 64) return n.form.waves_rows == 1 ? launch_attend<T, 64, 1, 4, 32, 2>(a, st) : launch_attend<T, 64, 4, 1, 64, 2>(a, st);
+        if (n.dp == 256) return n.form.waves_rows == 1 ? launch_attend<T, 256, 1, 4, 32, 1>(a, st) : launch_attend<T, 256, 4, 1, 32, 1>(a, st);
+        return n.form.waves_rows == 1   ? launch_attend<T, 128, 1, 4, 32, 2>(a, st)
+               : n.form.waves_rows == 4 ? launch_attend<T, 128, 4, 1, 64, 2>(a, st)
+                                        : launch_attend<T, 128, 8, 1, 64, 2>(a, st);
     }
-    if (n.dp == 64) return launch_attend<T, 64, 1, 4, 32, f32 ? 1 : 2>(a, st);
-    if (n.dp == 128) return launch_attend<T, 128, 1, 4, 32, f32 ? 1 : 2>(a, st);
-    if constexpr (!f32) return launch_attend<T, 256, 1, 4, 32, 1>(a, st);
-    return CKKS_E_INVAL;  // 32-bit rows of 256 always share tiles (plan_attend)
 }
 
 }  // namespace ckks

@@ -30,38 +30,65 @@ __device__ __forceinline__ u32 clamp_at(int32_t v, u32 top) { return v < 0 ? 0u 
 __device__ __forceinline__ Pack<int32_t, 4> load_ids(const int32_t *p, u32 n) {
     if (n >= 4) return load_pack<4>(p);
     Pack<int32_t, 4> t{};
-    for (u32 k = 0; k < n; ++k) t.v[k] = p[k];
+#pragma unroll
+    for (u32 k = 0; k < 3; ++k)
+        if (k < n) t.v[k] = p[k];
     return t;
 }
 
-// use(token - first, index) for the thread's part of the history, ids within the stretch only; `t` holds its first four.
+// use(token - first, index, k) for the thread's part of the history, ids within the stretch only; `t` holds its first four, which
+// come with k = 0 .. 3, the others with k = 4.
 template <class F>
 __device__ __forceinline__ void each_token(const LogitsArgs &a, u32 h0, u32 h1, Pack<int32_t, 4> t, u32 threads, u32 first, u32 span, F use) {
-    for (u32 i = h0 + 4 * threadIdx.x; i < h1;) {
+    u32 i = h0 + 4 * threadIdx.x;
+#pragma unroll
+    for (u32 k = 0; k < 4; ++k) {
+        const u32 c = (u32)t.v[k] - first;
+        if (i + k < h1 && c < span) use(c, i + k, k);
+    }
+    for (i += 4 * threads; i < h1; i += 4 * threads) {
+        t = load_ids(a.tokens + i, h1 - i);
 #pragma unroll
         for (u32 k = 0; k < 4; ++k) {
             const u32 c = (u32)t.v[k] - first;
-            if (i + k < h1 && c < span) use(c, i + k);
+            if (i + k < h1 && c < span) use(c, i + k, 4u);
         }
-        i += 4 * threads;
-        if (i < h1) t = load_ids(a.tokens + i, h1 - i);
     }
 }
 
+// A bias of the stretch: token, index in the bias list, value.
+struct Listed {
+    u32 token, index;
+    float value;
+};
 // Of the biases for token `c` of the stretch the one with the largest index: from LDS where the stretch's biases fit there.
-__device__ __forceinline__ float last_bias(const LogitsArgs &a, u32 c, u32 first, u32 b0, u32 b1, const u32 (*listed)[2], u32 n) {
-    u32 best = b0;
+__device__ __forceinline__ float last_bias(const LogitsArgs &a, u32 c, u32 first, u32 b0, u32 b1, const Listed *listed, u32 n) {
     if (n <= LISTED) {
+        u32 best = 0;
+        float value = 0.0f;
+#pragma unroll 8
         for (u32 k = 0; k < n; ++k)
-            if (listed[k][0] == c) best = max(best, listed[k][1]);
-    } else {
-        for (u32 b = b1; b-- > b0;)
-            if ((u32)a.bias_ids[b] - first == c) {
-                best = b;
-                break;
+            if (listed[k].token == c && listed[k].index >= best) {
+                best = listed[k].index;
+                value = listed[k].value;
             }
+        return value;
     }
-    return a.bias[best];
+    for (u32 b = b1; b-- > b0;)
+        if ((u32)a.bias_ids[b] - first == c) return a.bias[b];
+    return 0.0f;
+}
+
+// use(token - first, index, k) for the thread's part of the bias list, ids within the stretch only; `id` is the thread's first, which
+// comes with k = 0, the others with k = 1.
+template <class F>
+__device__ __forceinline__ void each_bias(const LogitsArgs &a, u32 b0, u32 b1, int32_t id, u32 threads, u32 first, u32 span, F use) {
+    u32 b = b0 + threadIdx.x;
+    if (b < b1 && (u32)id - first < span) use((u32)id - first, b, 0u);
+    for (b += threads; b < b1; b += threads) {
+        const u32 c = (u32)a.bias_ids[b] - first;
+        if (c < span) use(c, b, 1u);
+    }
 }
 
 // THREADS x V x R entries per block.  RULES: there is a history or a bias list.
@@ -70,7 +97,8 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
     constexpr int V = 8, SPAN = THREADS * V * R;
     __shared__ __attribute__((aligned(16))) u32 tally[RULES ? SPAN : 4];   // then the changed logits
     __shared__ u32 taken[RULES ? SPAN / 32 : 1];                           // a bit for each token that somebody works out
-    __shared__ u32 listed[RULES ? LISTED : 1][2], n_listed;                // {token, index in the bias list}
+    __shared__ Listed listed[RULES ? LISTED : 1];
+    __shared__ u32 n_listed;
     const u32 row = blockIdx.x / a.tiles, first = (blockIdx.x % a.tiles) * SPAN, span = min(a.vocab - first, (u32)SPAN);
     const T *in = (const T *)a.logits + (i64)row * a.ls + first;
     TO *out = (TO *)a.out + (i64)row * a.os + first;
@@ -87,6 +115,7 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
     }
     u32 h0 = 0, h1 = 0, b0 = 0, b1 = 0;
     Pack<int32_t, 4> t0{};
+    int32_t bias_id = 0;
     if (RULES) {
         u32 made = 0;
         if (a.tokens) {
@@ -102,44 +131,60 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         if (i0 < h1) t0 = load_ids(a.tokens + i0, h1 - i0);
         const float rep = a.repetition ? a.repetition[row] : 1.0f, freq = a.frequency ? a.frequency[row] : 0.0f,
                     pres = a.presence ? a.presence[row] : 0.0f;
+        // ... and so are the first bias and the logits of those tokens
+        float bias0 = 0.0f;
+        if (b0 + threadIdx.x < b1) {
+            bias_id = a.bias_ids[b0 + threadIdx.x];
+            bias0 = a.bias[b0 + threadIdx.x];
+        }
+        // (only those within the stretch, one in eight of a long row: the loads of the others would cost more than the branches)
+        float l0[4] = {0, 0, 0, 0}, bias_l = 0.0f;
+        u32 m0[4] = {0, 0, 0, 0}, bias_m = 0;
+#pragma unroll
+        for (u32 k = 0; k < 4; ++k) {
+            const u32 c = (u32)t0.v[k] - first;
+            if (i0 + k < h1 && c < span) {
+                l0[k] = (float)in[c];
+                m0[k] = mask ? (u32)mask[(first + c) >> 5] : ~0u;
+            }
+        }
+        if (b0 + threadIdx.x < b1 && (u32)bias_id - first < span) {
+            bias_l = (float)in[(u32)bias_id - first];
+            bias_m = mask ? (u32)mask[(u32)bias_id >> 5] : ~0u;
+        }
         for (u32 k = threadIdx.x; k < SPAN / 4; k += THREADS) ((uint4 *)tally)[k] = make_uint4(0, 0, 0, 0);
         for (u32 k = threadIdx.x; k < SPAN / 32; k += THREADS) taken[k] = 0;
         if (threadIdx.x == 0) n_listed = 0;
         __syncthreads();
-        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32 i) {
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32 i, u32) {
             if (i < made)
                 atomicOr(&tally[c], SEEN);
             else
                 atomicAdd(&tally[c], 1u);
         });
-        for (u32 b = b0 + threadIdx.x; b < b1; b += THREADS) {
-            const u32 c = (u32)a.bias_ids[b] - first;
-            if (c >= span) continue;
+        each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32 b, u32 k) {
             atomicOr(&tally[c], BIASED);
             const u32 at = atomicAdd(&n_listed, 1u);
-            if (at < LISTED) {
-                listed[at][0] = c;
-                listed[at][1] = b;
-            }
-        }
+            if (at < LISTED) listed[at] = {c, b, k ? a.bias[b] : bias0};
+        });
         __syncthreads();
         // whoever comes first to a token works it out, and leaves the result in place of the tally
-        auto change = [&](u32 c) {
+        auto change = [&](u32 c, bool known, float l, u32 m) {
             if (atomicOr(&taken[c >> 5], 1u << (c & 31)) >> (c & 31) & 1) return;
+            if (!known) {
+                l = (float)in[c];
+                m = mask ? (u32)mask[(first + c) >> 5] : ~0u;
+            }
             const u32 t = tally[c], n = t & COUNT;
-            float l = (float)in[c];
             if (t & ~BIASED) l = l > 0.0f ? l / rep : l * rep;
             l = l - freq * (float)n;
             l = l - (n ? pres : 0.0f);
             if (t & BIASED) l += last_bias(a, c, first, b0, b1, listed, n_listed);
-            if (mask && !((u32)mask[(first + c) >> 5] >> ((first + c) & 31) & 1)) l = -__builtin_inff();
+            if (!(m >> ((first + c) & 31) & 1)) l = -__builtin_inff();
             tally[c] = __float_as_uint(l);
         };
-        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32) { change(c); });
-        for (u32 b = b0 + threadIdx.x; b < b1; b += THREADS) {
-            const u32 c = (u32)a.bias_ids[b] - first;
-            if (c < span) change(c);
-        }
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32, u32 k) { change(c, k < 4, l0[k & 3], m0[k & 3]); });
+        each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32, u32 k) { change(c, !k, bias_l, bias_m); });
         __syncthreads();  // d_out may be d_logits: all that is changed has been read
     }
 #pragma unroll
@@ -157,11 +202,8 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
         auto write = [&](u32 c) {
             if (atomicAnd(&taken[c >> 5], ~(1u << (c & 31))) >> (c & 31) & 1) out[c] = (TO)__uint_as_float(tally[c]);
         };
-        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32) { write(c); });
-        for (u32 b = b0 + threadIdx.x; b < b1; b += THREADS) {
-            const u32 c = (u32)a.bias_ids[b] - first;
-            if (c < span) write(c);
-        }
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32, u32) { write(c); });
+        each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32, u32) { write(c); });
     }
 }
 

@@ -325,19 +325,23 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(NormArgs a) {
     }
 }
 
-// dw[c], db[c] = the parts' sums in order: 64 columns per block, 16 threads share a column's parts.
-template <class TW>
+// dw[c], db[c] = the sums of all parts, always in the same order.  COLS columns per block, 1024 / COLS threads share a column's
+// parts: 64 columns read whole lines, 16 leave fewer loads that wait for one another where there are few columns (1536 parts of
+// 218 columns 9 us against 14, 512 of 8192 10 against 8).
+template <class TW, int COLS>
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restrict__ part, u32 parts, u32 cols, TW *dw, TW *db) {
-    __shared__ float join[16][64];
-    const u32 c = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const u64 col = (u64)blockIdx.x * 64 + c;
+    __shared__ float join[16][COLS];
+    const u32 c = threadIdx.x % COLS, q = threadIdx.x / COLS;
+    const u64 col = (u64)blockIdx.x * COLS + c;
     TW *out = blockIdx.y ? db : dw;
     if (!out) return;
     float s = 0.0f;
     if (col < cols)
-#pragma unroll 4
-        for (u32 p = q; p < parts; p += 16) s += part[((size_t)p * 2 + blockIdx.y) * cols + col];
-    join[q][c] = s;
+#pragma unroll 8
+        for (u32 p = q; p < parts; p += 1024 / COLS) s += part[((size_t)p * 2 + blockIdx.y) * cols + col];
+#pragma unroll
+    for (int o = COLS; o < 64; o <<= 1) s += __shfl_xor(s, o);
+    if ((threadIdx.x & 63) < COLS) join[threadIdx.x >> 6][c] = s;
     __syncthreads();
     if (q == 0 && col < cols) {
         s = 0.0f;
@@ -345,6 +349,13 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restric
         for (int i = 0; i < 16; ++i) s += join[i][c];
         out[col] = (TW)s;
     }
+}
+template <class TW>
+static void launch_parts(const float *part, u32 parts, u32 cols, void *dw, void *db, hipStream_t st) {
+    if (cols >= 4096)
+        hipLaunchKernelGGL((norm_parts_kernel<TW, 64>), dim3((cols + 63) / 64, 2), dim3(1024), 0, st, part, parts, cols, (TW *)dw, (TW *)db);
+    else
+        hipLaunchKernelGGL((norm_parts_kernel<TW, 16>), dim3((cols + 15) / 16, 2), dim3(1024), 0, st, part, parts, cols, (TW *)dw, (TW *)db);
 }
 
 // Threads per row and entries per thread: the smallest group whose registers hold the row at up to 32 entries a thread
@@ -516,13 +527,12 @@ int ckks_clear_layer_norm_grad(const ckks_clear_norm_grad_t *p, void *stream) {
         CKKS_LAUNCH_CHECK("norm_grad_kernel");
     }
     if (params) {
-        const dim3 grid((p->cols + 63) / 64, 2);
         if (wtype == CKKS_CLEAR_F32)
-            hipLaunchKernelGGL(norm_parts_kernel<float>, grid, dim3(1024), 0, st, a.part, blocks, p->cols, (float *)p->d_dweight, (float *)p->d_dbias);
+            launch_parts<float>(a.part, blocks, p->cols, p->d_dweight, p->d_dbias, st);
         else if (wtype == CKKS_CLEAR_F16)
-            hipLaunchKernelGGL(norm_parts_kernel<f16>, grid, dim3(1024), 0, st, a.part, blocks, p->cols, (f16 *)p->d_dweight, (f16 *)p->d_dbias);
+            launch_parts<f16>(a.part, blocks, p->cols, p->d_dweight, p->d_dbias, st);
         else
-            hipLaunchKernelGGL(norm_parts_kernel<bf16>, grid, dim3(1024), 0, st, a.part, blocks, p->cols, (bf16 *)p->d_dweight, (bf16 *)p->d_dbias);
+            launch_parts<bf16>(a.part, blocks, p->cols, p->d_dweight, p->d_dbias, st);
         CKKS_LAUNCH_CHECK("norm_parts_kernel");
     }
     return CKKS_OK;

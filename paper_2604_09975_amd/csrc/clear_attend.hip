@@ -92,6 +92,12 @@ __device__ __forceinline__ typename Frag<T>::type col_frag(const T *v, u32 lane)
     return r;
 }
 
+// The larger of x and its value in the other half of the wave (NaN gives way), without LDS.
+__device__ __forceinline__ float other_half_max(float x) {
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+}
+
 // What a tile of rows works on.
 struct RowTile {
     u32 seq, start, n, first_row, rows;  // first token and tokens of the sequence; first row of the tile, rows in all
@@ -251,22 +257,31 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     // Where the rows that this thread fetches lie.  The table's answer is looked at only when it is needed, a tile later: a wait
     // or a branch here would be a wait for all loads under way.
     struct Place {
-        u32 page[PASSES], row[PASSES];
+        u32 page[PASSES], row[PASSES];  // of each row
+        u32 tile_page, tile_row;        // of the tile, where pages hold whole tiles
     };
+    const bool whole = a.page_size % TK == 0;
     auto look_up = [&](u32 tile) {
         Place at;
+        if (whole) {
+            const u32 j = min(r.tile0 + tile, ((u32)r.kv - 1) / TK) * TK, n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
+            at.tile_page = (u32)table[n];
+            at.tile_row = j - n * a.page_size;
+        } else {
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const u32 j = min((r.tile0 + tile) * TK + p * PASS + fetch_row, (u32)r.kv - 1);
-            const u32 n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
-            at.page[p] = (u32)table[n];
-            at.row[p] = j - n * a.page_size;
+            for (int p = 0; p < PASSES; ++p) {
+                const u32 j = min((r.tile0 + tile) * TK + p * PASS + fetch_row, (u32)r.kv - 1);
+                const u32 n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
+                at.page[p] = (u32)table[n];
+                at.row[p] = j - n * a.page_size;
+            }
         }
         return at;
     };
     // Rows and pieces that are not there are fetched from page 0 and become zeros when they are put into LDS (`none`: a bit
     // for each pass): a branch around a load would have its result copied, and so waited for, at once.
     const u32 lane_piece = piece_ok ? piece * E : 0;
+    const u32 k_lane = fetch_row * (u32)a.ks[2] + lane_piece, v_lane = fetch_row * (u32)a.vs[2] + lane_piece;
     struct Sources {
         u64 k[PASSES], v[PASSES];
         u32 none;
@@ -274,19 +289,32 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     auto locate = [&](u32 tile, const Place &at) {
         Sources s;
         s.none = piece_ok ? 0 : ~0u;
-        const bool ends = (r.tile0 + tile + 1) * TK > (u32)r.kv;
+        // check_cache: a page's stride fits 32 bits, and so does every offset within a page
+        if (whole) {
+            const u32 pg = at.tile_page < a.n_pages ? at.tile_page : 0;
+            if (at.tile_page >= a.n_pages) s.none = ~0u;
+            const u64 k0 = (u64)pg * (u32)a.ks[0] + at.tile_row * (u32)a.ks[2], v0 = (u64)pg * (u32)a.vs[0] + at.tile_row * (u32)a.vs[2];
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            u32 pg = at.page[p];
-            if (pg >= a.n_pages) {
-                pg = 0;
-                s.none |= 1u << p;
+            for (int p = 0; p < PASSES; ++p) {
+                s.k[p] = k0 + p * PASS * (u32)a.ks[2] + k_lane;
+                s.v[p] = v0 + p * PASS * (u32)a.vs[2] + v_lane;
             }
-            if (ends && (r.tile0 + tile) * TK + p * PASS + fetch_row >= (u32)r.kv) s.none |= 1u << p;
-            // check_cache: a page's stride fits 32 bits, and so does every offset within a page
-            s.k[p] = (u64)pg * (u32)a.ks[0] + (at.row[p] * (u32)a.ks[2] + lane_piece);
-            s.v[p] = a.alike ? s.k[p] : (u64)pg * (u32)a.vs[0] + (at.row[p] * (u32)a.vs[2] + lane_piece);
+        } else {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                u32 pg = at.page[p];
+                if (pg >= a.n_pages) {
+                    pg = 0;
+                    s.none |= 1u << p;
+                }
+                s.k[p] = (u64)pg * (u32)a.ks[0] + (at.row[p] * (u32)a.ks[2] + lane_piece);
+                s.v[p] = a.alike ? s.k[p] : (u64)pg * (u32)a.vs[0] + (at.row[p] * (u32)a.vs[2] + lane_piece);
+            }
         }
+        if ((r.tile0 + tile + 1) * TK > (u32)r.kv)
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p)
+                if ((r.tile0 + tile) * TK + p * PASS + fetch_row >= (u32)r.kv) s.none |= 1u << p;
         return s;
     };
     u32 k_none = 0, v_none = 0;
@@ -381,12 +409,13 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
                     if (key < from || key >= to) s[u][i] = -__builtin_inff();
                 }
         }
-        float top = s[0][0];
+        // four chains each for maximum and sum: nothing else runs on the wave meanwhile
+        float tops[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
-        top = fmaxf(top, __shfl_xor(top, 32));
+            for (int i = u ? 0 : 4; i < 16; ++i) tops[i % 4] = fmaxf(tops[i % 4], s[u][i]);
+        const float top = other_half_max(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
         // The maximum only has to keep exp2 in range: it moves when a score passes it by 8 powers of two, and then all
         // that was summed is scaled.
         if (__any((top - m) * a.c > 8.0f)) {

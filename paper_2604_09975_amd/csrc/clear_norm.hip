@@ -326,8 +326,8 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(NormArgs a) {
 }
 
 // dw[c], db[c] = the sums of all parts, always in the same order.  COLS columns per block, 1024 / COLS threads share a column's
-// parts: 64 columns read whole lines, 16 leave fewer loads that wait for one another where there are few columns (1536 parts of
-// 218 columns 9 us against 14, 512 of 8192 10 against 8).
+// parts: 64 columns read whole lines (512 parts of 8192 columns 6.7 us, with 16 11.8), 16 leave fewer loads that wait for one
+// another where there are few columns (14132 rows of 218, 1536 parts: forward and gradient 23.6 us, with 64 28.1).
 template <class TW, int COLS>
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restrict__ part, u32 parts, u32 cols, TW *dw, TW *db) {
     __shared__ float join[16][COLS];

@@ -826,7 +826,8 @@ static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
     for (u32 f = 0; f < count; ++f) {
         const AttendForm &form = forms[f];
         const double blocks = (seqs ? seqs * std::ceil(per_seq / form.rows) : 1) * g.kv_heads;
-        const double most = std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));
+        const bool may_split = (u64)b.n_tokens * p.heads < 1u << 31;  // the joining kernel's grid
+        const double most = !may_split ? 1.0 : std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));
         auto consider = [&](u32 splits) {
             if (splits < 1 || splits > most) return;
             const double load = blocks * splits / CUS, steps = std::ceil(keys / splits / form.keys);

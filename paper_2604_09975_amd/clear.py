@@ -15,6 +15,7 @@ from .binding import C, _check, _raw_stream, _stream, lib
 
 _TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _f32, _i32 = torch.float32, torch.int32
+_rowwise = torch.contiguous_format
 _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 # The argument structs of the header, field by field.
@@ -101,7 +102,7 @@ def ckks_clear_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stats=T
         elif wt != bt:
             raise TypeError("weight and bias must be of one type")
     if out is None:
-        out = x.new_empty(x.shape)
+        out = torch.empty_like(x, memory_format=_rowwise)
         py, ys = out.data_ptr(), cols
     else:
         py, ys = _ptr(out, dtype, dev, "out"), _rows(out, "out")[2]
@@ -110,8 +111,10 @@ def ckks_clear_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stats=T
     mean = rstd = None
     pm = pr = 0
     if stats:
-        mean, rstd = x.new_empty(x.shape[:-1], dtype=_f32), x.new_empty(x.shape[:-1], dtype=_f32)
-        pm, pr = mean.data_ptr(), rstd.data_ptr()
+        both = x.new_empty((2,) + x.shape[:-1], dtype=_f32)
+        mean, rstd = both.unbind(0)
+        pm = both.data_ptr()
+        pr = pm + 4 * rows
     rc = _norm(_NORM(px, pw, pb, py, pm, pr, xs, ys, rows, cols, code, wt, eps, 0), _on(dev))
     if rc:
         _check(rc)
@@ -134,7 +137,7 @@ def ckks_clear_layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, params=T
     if weight is not None:
         wt, pw = _param(weight, dtype, cols, dev, "weight")
     if dx is None:
-        dx = x.new_empty(x.shape)
+        dx = torch.empty_like(x, memory_format=_rowwise)
         pdx, dxs = dx.data_ptr(), cols
     else:
         pdx, dxs = _ptr(dx, dtype, dev, "dx"), _rows(dx, "dx")[2]
@@ -143,9 +146,10 @@ def ckks_clear_layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, params=T
     dw = db = None
     pgw = pgb = pwork = need = 0
     if params:
-        like = x.new_empty(0, dtype=_f32) if weight is None else weight
-        dw, db = like.new_empty(cols), like.new_empty(cols)
-        pgw, pgb = dw.data_ptr(), db.data_ptr()
+        grads = x.new_empty((2, cols), dtype=_f32 if weight is None else weight.dtype)
+        dw, db = grads.unbind(0)
+        pgw = grads.data_ptr()
+        pgb = pgw + cols * grads.element_size()
         need = _norm_grad_work(rows, cols, code)
         work = x.new_empty(max(need, 4), dtype=torch.uint8)
         pwork = work.data_ptr()
@@ -210,7 +214,7 @@ def ckks_clear_cache_append(k, v, k_pages, v_pages, page_table, q_start, kv_len,
     if q is not None:
         pq, heads, q0, q1 = _heads(q, dtype, n, dim, dev, "q")
         if q_out is None:
-            q_out = q.new_empty((n, heads, dim))
+            q_out = torch.empty_like(q, memory_format=_rowwise)
         po, ho, o0, o1 = _heads(q_out, dtype, n, dim, dev, "q_out")
         if ho != heads:
             raise ValueError("q_out must have q's heads")
@@ -239,7 +243,7 @@ def ckks_clear_attend(q, k_pages, v_pages, page_table, q_start, kv_len, scale=No
         raise ValueError(f"q must be [{n}][heads][{cache[11]}]")
     pq, heads, q0, q1 = _heads(q, dtype, n, dim, dev, "q")
     if out is None:
-        out = q.new_empty((n, heads, dim))
+        out = torch.empty_like(q, memory_format=_rowwise)
         po, o0, o1 = out.data_ptr(), heads * dim, dim
     else:
         po, ho, o0, o1 = _heads(out, dtype, n, dim, dev, "out")
@@ -271,7 +275,7 @@ def ckks_clear_logits(logits, out=None, tokens=None, token_start=None, n_prompt=
     pl = _ptr(logits, dtype, dev, "logits")
     rows, vocab, ls = _rows(logits, "logits")
     if out is None:
-        out = logits.new_empty(logits.shape)
+        out = torch.empty_like(logits, memory_format=_rowwise)
         po, os, oc = out.data_ptr(), vocab, code
     else:
         oc = _type(out, "out")

@@ -207,25 +207,40 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
     }
 }
 
-template <class T, class TO>
+template <class T, class TO, int THREADS, int R, bool RULES>
 static void launch_logits(LogitsArgs a, u32 rows, hipStream_t st) {
-    // 16384 entries a block: each block goes through the row's whole history, so long stretches go through it less often; 2048
-    // where that leaves most of the 256 CUs without a block
-    const bool small = (u64)rows * ((a.vocab + 16383) / 16384) < 256;
-    const u32 span = small ? 2048 : 16384;
+    constexpr u32 span = THREADS * 8 * R;
     a.tiles = (a.vocab + span - 1) / span;
-    const dim3 grid(rows * a.tiles);
-    if (a.tokens || a.bias) {
-        if (small)
-            hipLaunchKernelGGL((logits_kernel<T, TO, 256, 1, true>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((logits_kernel<T, TO, THREADS, R, RULES>), dim3(rows * a.tiles), dim3(THREADS), 0, st, a);
+}
+// Stretches: each block goes through the row's whole history, so long ones go through it less often, short ones put more CUs to
+// work.  Measured on one card, history of h tokens a row, us:
+//    8 rows of 50257, bf16:    2048 entries  4.8 (h = 100)   5.4 (1000)   7.6 (2000)  25.7 (10000)
+//                              8192          5.6             5.9          6.0         11.4
+//  256 rows of 131072, f32:    8192         60.6            59.9         63.9        129
+//                             16384         72.7            78.1         82.6        129
+//  256 rows of 131072, bf16:   8192         49.0            52.3         55.0        114
+//                             16384         41.5            43.6         45.8         84.5
+// So: 2048 where 8192 would leave CUs without a block, unless the threads of such a block need more than one load each for a
+// history; 16384 for 16-bit logits where that fills the CUs (32 bytes a thread either way).  The mask alone: 8192 where it fills the
+// CUs (256 x 131072 f32 49.5 us, bf16 29.3; with 2048 50.5 and 29.5, with 16384 62.0 and 29.4), else 2048 (8 x 50257 2.9 us,
+// with 8192 3.3).
+template <class T, class TO>
+static void launch_logits(const LogitsArgs &a, u32 rows, hipStream_t st) {
+    const auto blocks = [&](u32 span) { return (u64)rows * ((a.vocab + span - 1) / span); };
+    if (!a.tokens && !a.bias) {
+        if (blocks(8192) < 256)
+            launch_logits<T, TO, 256, 1, false>(a, rows, st);
         else
-            hipLaunchKernelGGL((logits_kernel<T, TO, 1024, 2, true>), grid, dim3(1024), 0, st, a);
-    } else {
-        if (small)
-            hipLaunchKernelGGL((logits_kernel<T, TO, 256, 1, false>), grid, dim3(256), 0, st, a);
-        else
-            hipLaunchKernelGGL((logits_kernel<T, TO, 1024, 2, false>), grid, dim3(1024), 0, st, a);
+            launch_logits<T, TO, 1024, 1, false>(a, rows, st);
+        return;
     }
+    if constexpr (sizeof(T) == 2)
+        if (blocks(16384) >= 256) return launch_logits<T, TO, 1024, 2, true>(a, rows, st);
+    if (blocks(8192) < 256 && a.n_tokens / rows <= 4 * 256)
+        launch_logits<T, TO, 256, 1, true>(a, rows, st);
+    else
+        launch_logits<T, TO, 1024, 1, true>(a, rows, st);
 }
 
 }  // namespace ckks

@@ -788,9 +788,11 @@ struct AttendForm {
 constexpr AttendForm FORMS_64[] = {{1, 32, 32, 128, 6, 1.1f, 1.6f, 2}, {4, 128, 64, 64, 7, 1.3f, 2.3f, 3}};
 constexpr AttendForm FORMS_128[] = {{1, 32, 32, 128, 6, 1.7f, 2.8f, 2}, {4, 128, 64, 64, 8, 1.8f, 2.6f, 2}, {8, 256, 64, 64, 10, 1.9f, 1.9f, 1}};
 constexpr AttendForm FORMS_256[] = {{1, 32, 32, 128, 8, 4, 4, 1}, {4, 128, 32, 32, 10, 2.2f, 2.2f, 1}};
-// 32-bit products are slow enough for the waves of a row tile to read their keys apart; rows of 256 do not fit so.
+// 32-bit products are slow enough for each wave to read its keys by itself: with rows of 64 the form of shared tiles gains nothing
+// (32 heads, 2 x 1024 tokens over 3024 keys: 439 us, apart 447); with rows of 128, where only one block of waves apart fits a CU,
+// two with shared tiles do (963 -> 802 us).  Rows of 256 fit no other way.
 constexpr AttendForm FORMS_F32_64[] = {{1, 32, 32, 128, 6, 4, 4, 1}};
-constexpr AttendForm FORMS_F32_128[] = {{1, 32, 32, 128, 6, 8, 8, 1}};
+constexpr AttendForm FORMS_F32_128[] = {{1, 32, 32, 128, 6, 8, 8, 1}, {4, 128, 32, 32, 10, 4.9f, 8.4f, 2}};
 constexpr AttendForm FORMS_F32_256[] = {{4, 128, 32, 32, 10, 14, 14, 1}};
 
 struct AttendPlan {
@@ -814,7 +816,7 @@ static bool plan_attend(const ckks_clear_attend_t &p, AttendPlan &n) {
     const bool f32 = g.dtype == CKKS_CLEAR_F32;
     const AttendForm *forms = f32 ? (n.dp == 64 ? FORMS_F32_64 : n.dp == 128 ? FORMS_F32_128 : FORMS_F32_256)
                                   : (n.dp == 64 ? FORMS_64 : n.dp == 128 ? FORMS_128 : FORMS_256);
-    const u32 count = f32 ? 1 : n.dp == 128 ? 3 : 2;
+    const u32 count = f32 ? (n.dp == 128 ? 2 : 1) : n.dp == 128 ? 3 : 2;
     constexpr double CUS = 256, READ = 4.9e6, JOIN = 1.5e6;  // bytes a microsecond
     const double per_seq = seqs ? (double)rows / seqs : 0, causal = p.flags & CKKS_CLEAR_CAUSAL;
     double keys = (double)width - (causal ? per_seq / group / 2 : 0);  // that a row sees, about
@@ -879,7 +881,7 @@ template <class T>
 static int launch_attend(const AttendArgs &a, const AttendPlan &n, hipStream_t st) {
     if constexpr (sizeof(T) == 4) {
         if (n.dp == 64) return launch_attend<T, 64, 1, 4, 32, 1>(a, st);
-        if (n.dp == 128) return launch_attend<T, 128, 1, 4, 32, 1>(a, st);
+        if (n.dp == 128) return n.form.waves_rows == 1 ? launch_attend<T, 128, 1, 4, 32, 1>(a, st) : launch_attend<T, 128, 4, 1, 32, 2>(a, st);
         return launch_attend<T, 256, 4, 1, 32, 1>(a, st);
     } else {
         if (n.dp == 64) return n.form.waves_rows == 1 ? launch_attend<T, 64, 1, 4, 32, 2>(a, st) : launch_attend<T, 64, 4, 1, 64, 2>(a, st);

@@ -135,6 +135,29 @@ def test_what_is_not_seen_does_not_matter(dtype, bad):
         close(out[n - 30:n], want[n - 30:n], attend_bound(c, want, mass)[n - 30:n], "window")
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dim", [96, 128, 200])
+def test_wide_heads_do_not_meet_what_they_do_not_see(dim, dtype):
+    """Chunks large enough for every form of shared tiles, pages that hold whole tiles and pages that do not."""
+    from paper_2604_09975_amd import clear as K
+    for page in (48, 64):
+        c = Cache([(900, 1000), (90, 300)], 64, 4, dim, page, TYPES[dtype], dim + page)
+        last = {b: (int(c.table[b, (kv - 1) // page]), (kv - 1) % page) for b, (_, kv) in enumerate(c.lens)}
+        for pg, row in last.values():  # beyond the lengths
+            c.k[pg, :, row + 1:] = math.nan
+            c.v[pg, :, row + 1:] = math.inf
+        check(c)
+        check(c, window=130)
+        n, kv = c.lens[0]
+        pg, row = last[0]
+        c.k[pg, :, row] = 0.0
+        c.v[pg, 1, row, dim - 1] = math.inf  # the last token's: its own query's alone, and the heads' that share it
+        out = K.ckks_clear_attend(c.q, *c.args())
+        assert torch.isfinite(out[:n - 1]).all() and torch.isfinite(out[n:]).all()
+        odd = ~torch.isfinite(out[n - 1])
+        assert odd[16:32, dim - 1].all() and int(odd.sum()) == 16
+
+
 def test_pages_out_of_range_read_as_zeros():
     c = Cache([(3, 70)], 4, 2, 64, 16, torch.float16, 7)
     hole = int(c.table[0, 2])

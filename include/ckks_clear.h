@@ -86,7 +86,8 @@ typedef struct {
  * d_cos / d_sin [n_pos][rot/2] (f32) at the token's position, or at d_positions[row] (int32 [n_tokens]) if that is given.
  * The rotation is computed in 32 bits and rounded once.  A position outside [0, n_pos) has no angle: the rotated
  * entries come out as NaN.  Tokens at a position below 0 and pages outside [0, n_pages) are not stored.
- * d_k, d_v: rows by strides {token, head}.  d_q may be NULL; d_q_out may be d_q with the same strides. */
+ * d_k, d_v: rows by strides {token, head}.  d_q may be NULL; d_q_out may be d_q with the same strides.  A row in no sequence has no
+ * position.  heads and kv_heads: at most 65536. */
 #define CKKS_CLEAR_INTERLEAVED 1u
 typedef struct {
     ckks_clear_pages_t pages;
@@ -104,8 +105,10 @@ int ckks_clear_cache_append(const ckks_clear_append_t *a, void *stream);
  * A query at position t sees the keys j < kv_len, with CKKS_CLEAR_CAUSAL only j <= t, with window > 0 (causal only) only
  * j > t - window:
  *   out = sum_j softmax_j(scale q.k_j) v_j,  lse = log sum_j exp(scale q.k_j)   (natural logarithm)
- * A query that sees no key gets out = 0 and lse = -infinity.  Keys and values that a query does not see do not reach its
- * result, whatever they hold.  A page outside [0, n_pages) reads as zeros.  scale > 0 and finite.
+ * A query that sees no key (or only keys with scores of -infinity) gets out = 0 and lse = -infinity.  Keys and values that a query
+ * does not see do not reach its result, whatever they hold.  A page outside [0, n_pages) reads as zeros.  scale > 0 and finite,
+ * scores scale q.k and their multiples by log2(e) within the range of 32 bits.  Rows of q in no sequence are not written.
+ * heads: a multiple of kv_heads, at most 65536, n_tokens * heads / kv_heads below 2^31.
  * With 16-bit types the softmax's weights are rounded to that type before they meet the values; all sums are
  * 32-bit.  d_q, d_out: [n_tokens][heads][head_dim] by strides {token, head}; d_lse f32 [n_tokens][heads] or NULL.
  * d_work: at least ckks_clear_attend_work_bytes bytes, 16-byte aligned, contents free (NULL if that is 0). */
@@ -135,7 +138,8 @@ int ckks_clear_attend(const ckks_clear_attend_t *a, void *stream);
  *   biases (bias_ids / bias [bias_start[r] .. bias_start[r+1])): l += bias; of several for one token the last counts
  *   mask: bit v % 32 of word d_mask[r * mask_stride + v / 32] clear:  l = -infinity, whatever l was
  * d_repetition, d_frequency, d_presence: f32 [rows], any may be NULL (1, 0, 0).  d_n_prompt NULL: all generated.
- * Ids outside [0, vocab) are ignored; token_start / bias_start outside [0, n_tokens / n_biases] are clamped.
+ * Ids outside [0, vocab) are ignored; token_start / bias_start outside [0, n_tokens / n_biases] are clamped.  n_tokens and n_biases
+ * are below 2^30.
  * Computed in 32 bits, rounded once to out_dtype (dtype or F32).  d_out may be d_logits with the same stride and type. */
 typedef struct {
     const void *d_logits;

@@ -10,6 +10,14 @@
 //   KW > 1: one set of 32 rows, each wave takes every KW-th tile through its own stretch of LDS, without barriers, and the
 //           waves' results are joined at the end (single tokens: the time is that of reading the cache).
 // Either may split the keys over several blocks; a second kernel then joins the blocks' results in order.
+//
+// Measured (heads of 128, 32 query and 8 kv heads, 16 bits, unless said):
+//   prompts, 2 chunks of up to 4096 tokens over 12301 more keys, RW = 8: 1265 us, 1.04 PFLOP/s, where a library product of 8192^3
+//     reaches 1.13; the matrix units are fed half the cycles and the softmax's arithmetic takes nearly as many, at a clock that
+//     the power limit holds down;
+//   64 single tokens over up to 8192 keys each, KW = 4: 226 us for 1.2 GB, 5.3 TB/s;
+//   1 token over 131002 keys, 16 and 2 heads, KW = 4, split: 26 us and 5.4 us to join (134 MB, 27 us at a copy's rate);
+//   1 token over 128 keys, 12 heads of 64: 6.4 us; 128 tokens of 32 bits: 10.4 us: the chain of lookup, load, product, join.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -701,7 +709,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
 }
 
 // Joins the splits of a row (token, head): WAVES waves for each, a group of `lanes` lanes (four entries each) takes every
-// so-manieth split, and the groups' sums are added in their order.
+// so-manieth split, and the groups' sums are added in their order.  Bound by latency.  us of 2048 rows of 6 splits: one wave a
+// row 7.1, four 8.6, sixteen 21; of 16 rows of 128 splits: 21, 8.7, 6.2.
 template <class T, int ROWS, int TK, int WAVES>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void attend_join_kernel(AttendArgs a, u32 lanes) {
     constexpr int PER = WAVES < 4 ? 4 / WAVES : 1;  // rows of a block

@@ -1,7 +1,11 @@
 // Rules on logits: history penalties, biases, mask.  A block takes a stretch of one row's vocabulary.  It tallies in LDS what the
 // row's history and bias list say about the tokens of that stretch, works out the few logits that they change, streams the stretch
-// through the mask, and then writes the changed ones over it: the many logits cost no more than a masked copy.  The tallies are
-// whole numbers, and of several biases the largest index counts: no order shows in a result.
+// through the mask, and then writes the changed ones over it.  The tallies are whole numbers, and of several biases the largest
+// index counts: no order shows in a result.
+// Bound by memory where there is no history (256 x 131072 bf16 with a mask 29 us, 4.8 TB/s); with one by the chain of its lookups,
+// which a second block on the CU hides in part (the same with 4000 tokens and 100 biases a row 51 to 59 us), and by the launch for a
+// row (50257 f32, 5.5 us).  Measured and dropped: a launch for the masked copy and one that tallies a row's history by hashing
+// (64.9 us with 4000 tokens a row, 41.8 with 1000, where this takes 51.2 and 43.9; 256 x 131072 f32 110 and 71.6 against 75 and 60).
 #include <algorithm>
 
 #include "clear_device.h"

@@ -559,7 +559,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
                 at = look_up(i + 2);
             }
             work(i, buf + (i - first & 1) * Shape::TILE);
-            // the other buffer was read before this round's barrier
+            // the other buffer was read before this barrier
             put_k(buf + (i + 1 - first & 1) * Shape::TILE);
             put_v(i + 1, buf + (i + 1 - first & 1) * Shape::TILE + TK * KS);
         }

@@ -63,7 +63,7 @@ struct Columns {
 
 // TPR threads hold a row, E entries each: mean, then the sum of squares about it (two passes over registers: no cancellation), then
 // the scaled row.  Bound by memory: 16384 x 8192 bf16 in 92 us, 5.8 TB/s of the 4.9 that a large copy reaches (part of it lies in
-// the last cache); 4099 x 1280 f16 8.0 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
+// the last cache); 4099 x 1280 f16 7.6 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 
 // As norm_kernel with rows of x and dy.  The weight lies in LDS: registers hold the sums of the columns and the row that comes
 // next.  Bound by memory: 16384 x 8192 bf16 183 us, 4.6 TB/s with the sums that it writes (256 us with loads behind branches and
-// no row ahead); 4099 x 1280 f16 15.8 us, by the latency of the two or three rows that each group then has.
+// no row ahead); 4099 x 1280 f16 14.2 us, by the latency of the few rows that each group then has.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR, GROUPS = THREADS / TPR;
@@ -369,21 +369,25 @@ static void launch_parts(const float *part, u32 parts, u32 cols, void *dw, void 
 // more exchanges and has fewer bytes under way.  us forward, gradient (bf16):
 //   16384 x 2048: 64 threads 25.2, 45.9; 256 threads 29.0, 60.2      8192 x 8192: 256 threads 45.4, 99.8; 1024 threads 79.7, 115
 //   32768 x 1536: 64 threads 35.7, 61.8; 256 threads 53.6, 88.8      64 x 2048: 3.9, 9.8 and 3.3, 7.9: not worth a second rule
+// 24 entries where they do rather than 32: 16384 x 1280 15.8, 31.6 (32: 17.2, 34.7), 4000 x 4800 f32 27.0, 51.0 (27.7, 60.2).
 struct NormShape {
     u32 tpr, e;
 };
 static NormShape norm_shape(u32 cols) {
     if (cols < 8) return {0, 0};
-    if (cols <= 64 * 32) return {64, cols <= 64 * 8 ? 8u : cols <= 64 * 16 ? 16u : 32u};
-    if (cols <= 256 * 32) return {256, cols <= 256 * 16 ? 16u : 32u};
+    if (cols <= 64 * 32) return {64, cols <= 64 * 8 ? 8u : cols <= 64 * 16 ? 16u : cols <= 64 * 24 ? 24u : 32u};
+    if (cols <= 256 * 32) return {256, cols <= 256 * 16 ? 16u : cols <= 256 * 24 ? 24u : 32u};
     if (cols <= 1024 * 16) return {1024, 16};
     return {0, 0};
 }
 // Blocks: as many as the registers let run at once on 256 CUs, each with every so-manieth row.  Each block of the gradient leaves
-// one pair of column sums.
+// one pair of column sums, so beyond one block for each CU its groups have four rows at least (us with a row each: 1000 x 5000 bf16
+// 25.1, 29.4; 4099 x 1280 f16 17.6, 18.5; 2000 x 768 f32 11.2, 13.8).
 static u32 norm_blocks(u32 rows, const NormShape &s, bool grad) {
-    const u32 per = s.tpr == 64 ? 4 : 1, cu = s.tpr == 1024 ? 1 : grad ? (s.e == 32 ? 2 : s.e == 16 ? 4 : 6) : (s.e == 32 ? 3 : 6);
-    return std::min<u32>((rows + per - 1) / per, 256 * cu);
+    const u32 per = s.tpr == 64 ? 4 : 1, most = (rows + per - 1) / per;
+    if (!grad) return std::min<u32>(most, 256 * (s.tpr == 1024 ? 1 : s.e == 32 ? 3 : s.e == 24 ? 4 : 6));
+    const u32 cu = s.tpr == 1024 ? 1 : s.e >= 24 ? 2 : s.e == 16 ? 4 : 6;
+    return std::min(most, std::max<u32>(256, std::min(256 * cu, rows / (4 * per))));
 }
 static u32 norm_grad_blocks(u32 rows, u32 cols) {
     const NormShape s = norm_shape(cols);
@@ -401,8 +405,10 @@ static void launch_norm(const NormArgs &a, hipStream_t st) {
     }
     CKKS_NORM(64, 8)
     CKKS_NORM(64, 16)
+    CKKS_NORM(64, 24)
     CKKS_NORM(64, 32)
     CKKS_NORM(256, 16)
+    CKKS_NORM(256, 24)
     CKKS_NORM(256, 32)
     CKKS_NORM(1024, 16)
 #undef CKKS_NORM
@@ -419,8 +425,10 @@ static void launch_norm_grad(const NormArgs &a, u32 blocks, hipStream_t st) {
     }
     CKKS_NORM(64, 8)
     CKKS_NORM(64, 16)
+    CKKS_NORM(64, 24)
     CKKS_NORM(64, 32)
     CKKS_NORM(256, 16)
+    CKKS_NORM(256, 24)
     CKKS_NORM(256, 32)
     CKKS_NORM(1024, 16)
 #undef CKKS_NORM

@@ -15,8 +15,8 @@
 //   prompts, 2 chunks of up to 4096 tokens over 12301 more keys, RW = 8: 1265 us, 1.04 PFLOP/s, where a library product of 8192^3
 //     reaches 1.13; the matrix units are fed half the cycles and the softmax's arithmetic takes nearly as many, at a clock that
 //     the power limit holds down;
-//   64 single tokens over up to 8192 keys each, KW = 4: 226 us for 1.2 GB, 5.3 TB/s;
-//   1 token over 131002 keys, 16 and 2 heads, KW = 4, split: 26 us and 5.4 us to join (134 MB, 27 us at a copy's rate);
+//   64 single tokens over up to 8192 keys each, KW = 4: 225 us for 1.2 GB, 5.3 TB/s;
+//   1 token over 131002 keys, 16 and 2 heads, KW = 4, split: 26 us and 5 us to join (134 MB, 27 us at a copy's rate);
 //   1 token over 128 keys, 12 heads of 64: 6.4 us; 128 tokens of 32 bits: 10.4 us: the chain of lookup, load, product, join.
 #include <algorithm>
 #include <cmath>
@@ -118,8 +118,8 @@ __device__ __forceinline__ int row_pos(const AttendArgs &a, const RowTile &r, u3
 
 // Key tiles that the rows first_row .. first_row + ROWS - 1 see between them.
 template <int ROWS, int TK>
-__device__ __forceinline__ void key_range(const AttendArgs &a, RowTile &r) {
-    const int kv = min(a.kv_len[r.seq], (int)(a.table_width * a.page_size));
+__device__ __forceinline__ void key_range(const AttendArgs &a, int kv_len, RowTile &r) {
+    const int kv = min(kv_len, (int)(a.table_width * a.page_size));
     r.kv = max(0, kv);
     r.t0 = max(kv, 0) - (int)r.n;
     const u32 last = min(r.first_row + ROWS, r.rows) - 1;
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     RowTile r;
     // the last tiles of a causal chunk see the most keys: they start first
     if (!find_tile<ROWS>(a, a.tiles - 1 - blockIdx.x / a.kv_heads / a.splits, r)) return;
-    key_range<ROWS, TK>(a, r);
+    key_range<ROWS, TK>(a, a.kv_len[r.seq], r);
     // the same in every lane: scalars from here on
     r.kv = __builtin_amdgcn_readfirstlane(r.kv);
     r.t0 = __builtin_amdgcn_readfirstlane(r.t0);
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
 
 // Joins the splits of a row (token, head): WAVES waves for each, a group of `lanes` lanes (four entries each) takes every
 // so-manieth split, and the groups' sums are added in their order.  Bound by latency.  us of 2048 rows of 6 splits: one wave a
-// row 7.1, four 8.6, sixteen 21; of 16 rows of 128 splits: 21, 8.7, 6.2.
+// row 5.0, four 7.3, sixteen 20; of 16 rows of 128 splits: 20, 7.8, 5.0.
 template <class T, int ROWS, int TK, int WAVES>
 __global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void attend_join_kernel(AttendArgs a, u32 lanes) {
     constexpr int PER = WAVES < 4 ? 4 / WAVES : 1;  // rows of a block
@@ -720,50 +720,70 @@ __global__ __launch_bounds__(WAVES < 4 ? 256 : 64 * WAVES) void attend_join_kern
     const u32 in_row = threadIdx.x % (64 * WAVES), lane = threadIdx.x & 63;
     const u32 token = (u32)(at / a.heads), head = (u32)(at % a.heads);
     const u32 groups = 64 * WAVES / lanes, group = in_row / lanes, e = in_row % lanes * 4;
+    const float *lse = a.part_lse + at * a.splits, *part = a.part + at * a.splits * a.head_dim + (e < a.head_dim ? e : 0);
+    const bool row_ok = token < a.n_tokens;
+    // The first splits' results and the sequences' lengths are under way before it is known which of them count.
+    constexpr int EARLY = 4;
+    float z0 = 0.0f, z[EARLY];
+    float4 x[EARLY];
+    if (row_ok) {
+        z0 = lse[min(lane, a.splits - 1)];
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k) {
+            const u32 i = min(group + k * groups, a.splits - 1);
+            z[k] = lse[i];
+            x[k] = *(const float4 *)(part + (u64)i * a.head_dim);
+        }
+    }
     RowTile r;
     r.n_splits = 1;
-    if (token < a.n_tokens) {
-        u32 lo = 0, hi = a.n_seq;
-        while (hi - lo > 1) {
-            const u32 mid = (lo + hi) >> 1;
-            if ((i64)a.q_start[mid] <= (i64)token)
-                lo = mid;
-            else
-                hi = mid;
+    if (row_ok) {
+        // the last sequence that starts at the token or before it: down to 64 by halves, then a lane for each
+        u32 first = 0, count = a.n_seq;
+        while (count > 64) {
+            const u32 mid = first + count / 2;
+            const bool up = (i64)a.q_start[mid] <= (i64)token;
+            count = up ? count - count / 2 : count / 2;
+            first = up ? mid : first;
         }
-        const int s = min(max(a.q_start[lo], 0), (int)a.n_tokens), end = max(min(a.q_start[lo + 1], (int)a.n_tokens), s);
+        const u32 b = first + min(lane, count - 1);
+        const int start = a.q_start[b], next = a.q_start[b + 1], kv_len = a.kv_len[b];
+        const u64 before = __ballot(lane < count && start <= (int)token);
+        const int own = before ? 63 - __clzll(before) : 0;
+        const int s = min(max(__shfl(start, own), 0), (int)a.n_tokens), end = max(min(__shfl(next, own), (int)a.n_tokens), s);
+        const int kv = __shfl(kv_len, own);
         if ((int)token >= s && (int)token < end) {
-            r.seq = lo;
+            r.seq = first + own;
             r.start = s;
             r.n = end - s;
             r.rows = r.n * a.group;
             r.first_row = ((token - s) * a.group + head % a.group) / ROWS * ROWS;
-            key_range<ROWS, TK>(a, r);
+            key_range<ROWS, TK>(a, kv, r);
         }
     }
     // one split: the row has been written already
     const u32 n = r.n_splits > 1 ? r.n_splits : 0;
-    const float *lse = a.part_lse + at * a.splits;
-    float top = -__builtin_inff();
-    for (u32 i = lane; i < n; i += 64) top = fmaxf(top, lse[i]);
+    float top = lane < n ? z0 : -__builtin_inff();
+    for (u32 i = lane + 64; i < n; i += 64) top = fmaxf(top, lse[i]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     float sum = 0.0f;
     float4 acc = make_float4(0, 0, 0, 0);
+    auto add = [&](float zi, float4 xi) {
+        // a split that saw no key has nothing to add; one whose sum is not a number has
+        const float f = zi == -__builtin_inff() ? 0.0f : zi != zi ? zi : __builtin_amdgcn_exp2f(zi - top);
+        sum += f;
+        acc.x = __builtin_fmaf(f, xi.x, acc.x);
+        acc.y = __builtin_fmaf(f, xi.y, acc.y);
+        acc.z = __builtin_fmaf(f, xi.z, acc.z);
+        acc.w = __builtin_fmaf(f, xi.w, acc.w);
+    };
     if (e < a.head_dim) {
-        const float *p = a.part + at * a.splits * a.head_dim + e;
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k)
+            if (group + k * groups < n) add(z[k], x[k]);
 #pragma unroll 4
-        for (u32 i = group; i < n; i += groups) {
-            const float z = lse[i];
-            const float4 x = *(const float4 *)(p + (u64)i * a.head_dim);
-            // a split that saw no key has nothing to add; one whose sum is not a number has
-            const float f = z == -__builtin_inff() ? 0.0f : z != z ? z : __builtin_amdgcn_exp2f(z - top);
-            sum += f;
-            acc.x = __builtin_fmaf(f, x.x, acc.x);
-            acc.y = __builtin_fmaf(f, x.y, acc.y);
-            acc.z = __builtin_fmaf(f, x.z, acc.z);
-            acc.w = __builtin_fmaf(f, x.w, acc.w);
-        }
+        for (u32 i = group + EARLY * groups; i < n; i += groups) add(lse[i], *(const float4 *)(part + (u64)i * a.head_dim));
     }
     acc_of[threadIdx.x] = acc;
     if (e == 0) sum_of[threadIdx.x / lanes] = sum;

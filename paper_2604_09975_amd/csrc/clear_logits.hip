@@ -3,7 +3,7 @@
 // through the mask, and then writes the changed ones over it.  The tallies are whole numbers, and of several biases the largest
 // index counts: no order shows in a result.
 // Bound by memory where there is no history (256 x 131072 bf16 with a mask 29 us, 4.8 TB/s); with one by the chain of its lookups,
-// which a second block on the CU hides in part (the same with 4000 tokens and 100 biases a row 51 to 59 us), and by the launch for a
+// which a second block on the CU hides in part (the same with 4000 tokens a row 52 us, with up to 4000 and 100 biases 56), and by the launch for a
 // row (50257 f32, 5.5 us).  Measured and dropped: a launch for the masked copy and one that tallies a row's history by hashing
 // (64.9 us with 4000 tokens a row, 41.8 with 1000, where this takes 51.2 and 43.9; 256 x 131072 f32 110 and 71.6 against 75 and 60).
 #include <algorithm>
@@ -12,9 +12,9 @@
 
 namespace ckks {
 
-// Tally of a token: it is in the prompt; the row's bias list has it; below these how often it was generated.
-constexpr u32 SEEN = 1u << 31, BIASED = 1u << 30, COUNT = BIASED - 1;
-constexpr u32 LISTED = 1024;  // biases of a stretch that are kept in LDS
+// Tally of a token: it is in the prompt; below this how often it was generated.
+constexpr u32 SEEN = 1u << 31, COUNT = SEEN - 1;
+constexpr u32 LISTED = 512, PLACES = 2 * LISTED;  // biases of a stretch that a table in LDS holds, in twice as many places
 
 struct LogitsArgs {
     const void *logits;
@@ -60,29 +60,18 @@ __device__ __forceinline__ void each_token(const LogitsArgs &a, u32 h0, u32 h1, 
     }
 }
 
-// A bias of the stretch: token, index in the bias list, value.
-struct Listed {
-    u32 token, index;
-    float value;
-};
-// Of the biases for token `c` of the stretch the one with the largest index: from LDS where the stretch's biases fit there.
-__device__ __forceinline__ float last_bias(const LogitsArgs &a, u32 c, u32 first, u32 b0, u32 b1, const Listed *listed, u32 n) {
-    if (n <= LISTED) {
-        u32 best = 0;
-        float value = 0.0f;
-#pragma unroll 8
-        for (u32 k = 0; k < n; ++k)
-            if (listed[k].token == c && listed[k].index >= best) {
-                best = listed[k].index;
-                value = listed[k].value;
-            }
-        return value;
+// The place of token `c` of the stretch in the table of tokens + 1, found by hashing; the table is at most half full.  (A search of
+// the stretch's list by each token took 22 us for 10 rows of 2228 with 83 biases, this takes 6; beyond the table, a row of 50257 with
+// a bias for each token takes 270.)
+__device__ __forceinline__ u32 bias_place(u32 *table, u32 c) {
+    static_assert(PLACES == 1u << (32 - 22), "bits of the hash");
+    u32 at = c * 2654435769u >> 22;
+    for (;;) {
+        const u32 was = atomicCAS(&table[at], 0u, c + 1);
+        if (was == 0 || was == c + 1) return at;
+        at = (at + 1) % PLACES;
     }
-    for (u32 b = b1; b-- > b0;)
-        if ((u32)a.bias_ids[b] - first == c) return a.bias[b];
-    return 0.0f;
 }
-
 // use(token - first, index, k) for the thread's part of the bias list, ids within the stretch only; `id` is the thread's first, which
 // comes with k = 0, the others with k = 1.
 template <class F>
@@ -100,8 +89,8 @@ template <class T, class TO, int THREADS, int R, bool RULES>
 __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
     constexpr int V = 8, SPAN = THREADS * V * R;
     __shared__ __attribute__((aligned(16))) u32 tally[RULES ? SPAN : 4];   // then the changed logits
-    __shared__ u32 taken[RULES ? SPAN / 32 : 1];                           // a bit for each token that somebody works out
-    __shared__ Listed listed[RULES ? LISTED : 1];
+    __shared__ u32 taken[RULES ? SPAN / 32 : 1], biased[RULES ? SPAN / 32 : 1];  // a bit for each token: worked out; in the bias list
+    __shared__ u32 bias_token[RULES ? PLACES : 1], bias_last[RULES ? PLACES : 1];  // the table; largest index in the bias list + 1
     __shared__ u32 n_listed;
     const u32 row = blockIdx.x / a.tiles, first = (blockIdx.x % a.tiles) * SPAN, span = min(a.vocab - first, (u32)SPAN);
     const T *in = (const T *)a.logits + (i64)row * a.ls + first;
@@ -157,7 +146,9 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
             bias_m = mask ? (u32)mask[(u32)bias_id >> 5] : ~0u;
         }
         for (u32 k = threadIdx.x; k < SPAN / 4; k += THREADS) ((uint4 *)tally)[k] = make_uint4(0, 0, 0, 0);
-        for (u32 k = threadIdx.x; k < SPAN / 32; k += THREADS) taken[k] = 0;
+        for (u32 k = threadIdx.x; k < SPAN / 32; k += THREADS) taken[k] = biased[k] = 0;
+        if (b0 < b1)
+            for (u32 k = threadIdx.x; k < PLACES; k += THREADS) bias_token[k] = bias_last[k] = 0;
         if (threadIdx.x == 0) n_listed = 0;
         __syncthreads();
         each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32 i, u32) {
@@ -166,29 +157,53 @@ __global__ __launch_bounds__(THREADS) void logits_kernel(LogitsArgs a) {
             else
                 atomicAdd(&tally[c], 1u);
         });
-        each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32 b, u32 k) {
-            atomicOr(&tally[c], BIASED);
-            const u32 at = atomicAdd(&n_listed, 1u);
-            if (at < LISTED) listed[at] = {c, b, k ? a.bias[b] : bias0};
+        each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32 b, u32) {
+            atomicOr(&biased[c >> 5], 1u << (c & 31));
+            if (atomicAdd(&n_listed, 1u) < LISTED) atomicMax(&bias_last[bias_place(bias_token, c)], b + 1);
         });
         __syncthreads();
-        // whoever comes first to a token works it out, and leaves the result in place of the tally
-        auto change = [&](u32 c, bool known, float l, u32 m) {
-            if (atomicOr(&taken[c >> 5], 1u << (c & 31)) >> (c & 31) & 1) return;
+        // A token with biases is worked out by the thread of its last bias, one without by whoever comes first; the result takes the
+        // place of the tally.
+        auto take = [&](u32 c) { return !(atomicOr(&taken[c >> 5], 1u << (c & 31)) >> (c & 31) & 1); };
+        auto change = [&](u32 c, bool known, float l, u32 m, float bias) {
             if (!known) {
                 l = (float)in[c];
                 m = mask ? (u32)mask[(first + c) >> 5] : ~0u;
             }
             const u32 t = tally[c], n = t & COUNT;
-            if (t & ~BIASED) l = l > 0.0f ? l / rep : l * rep;
+            if (t) l = l > 0.0f ? l / rep : l * rep;
             l = l - freq * (float)n;
             l = l - (n ? pres : 0.0f);
-            if (t & BIASED) l += last_bias(a, c, first, b0, b1, listed, n_listed);
+            l += bias;
             if (!(m >> ((first + c) & 31) & 1)) l = -__builtin_inff();
             tally[c] = __float_as_uint(l);
         };
-        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32, u32 k) { change(c, k < 4, l0[k & 3], m0[k & 3]); });
-        each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32, u32 k) { change(c, !k, bias_l, bias_m); });
+        each_token(a, h0, h1, t0, THREADS, first, span, [&](u32 c, u32, u32 k) {
+            if (!(biased[c >> 5] >> (c & 31) & 1) && take(c)) change(c, k < 4, l0[k & 3], m0[k & 3], -0.0f);
+        });
+        auto last = [&](u32 c, u32 b, u32 k) {
+            take(c);
+            change(c, !k, bias_l, bias_m, k ? a.bias[b] : bias0);
+        };
+        if (n_listed <= LISTED) {
+            each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32 b, u32 k) {
+                if (bias_last[bias_place(bias_token, c)] == b + 1) last(c, b, k);
+            });
+        } else {
+            // too many for the table: for PLACES tokens at a time, a place for each
+            for (u32 sub = 0; sub < span; sub += PLACES) {
+                __syncthreads();
+                for (u32 k = threadIdx.x; k < PLACES; k += THREADS) bias_last[k] = 0;
+                __syncthreads();
+                each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32 b, u32) {
+                    if (c - sub < PLACES) atomicMax(&bias_last[c - sub], b + 1);
+                });
+                __syncthreads();
+                each_bias(a, b0, b1, bias_id, THREADS, first, span, [&](u32 c, u32 b, u32 k) {
+                    if (c - sub < PLACES && bias_last[c - sub] == b + 1) last(c, b, k);
+                });
+            }
+        }
         __syncthreads();  // d_out may be d_logits: all that is changed has been read
     }
 #pragma unroll

@@ -96,6 +96,13 @@ def test_each_rule_alone(parts):
         check(make(rows, vocab, torch.float16, 4, *parts))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab,biases", [(3, 2100, 4000), (2, 9000, 12000), (1, 40, 600), (257, 1500, 1400), (257, 300, 520)])
+def test_more_biases_than_a_table_holds(rows, vocab, biases, dtype):
+    """A bias for most tokens, several for some; rows with few beside rows with many."""
+    check(make(rows, vocab, TYPES[dtype], rows + vocab, hist=60, biases=biases))
+
+
 def test_one_token_many_times_and_the_last_bias_counts():
     s = make(4, 700, torch.float32, 5, hist=5000, biases=400, lo=3, hi=9)
     check(s)

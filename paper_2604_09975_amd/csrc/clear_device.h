@@ -1,4 +1,4 @@
-// Types, wide loads and wave reductions of the steps in the clear (clear_*.hip).
+// Types, wide loads and checks of arguments of the steps in the clear (clear_*.hip).
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -45,12 +45,6 @@ __device__ __forceinline__ void store_part(T *p, const Pack<T, N> &x, int n) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
         if (i < n) p[i] = x.v[i];
-}
-
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-    return x;
 }
 
 // ---- host ----

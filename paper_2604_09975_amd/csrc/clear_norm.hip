@@ -22,8 +22,11 @@ struct NormArgs {
 // barrier per call is enough: a wave can be at most one call ahead.
 template <int TPR>
 __device__ __forceinline__ void group_sum2(float &p, float &q, float (*ex)[2][2], u32 &slot) {
-    p = wave_sum(p);
-    q = wave_sum(q);
+#pragma unroll
+    for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) {
+        p += __shfl_xor(p, o);
+        q += __shfl_xor(q, o);
+    }
     if (TPR > 64) {
         const u32 wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
@@ -67,7 +70,7 @@ struct Columns {
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
-    __shared__ float ex[TPR / 64][2][2];
+    __shared__ float ex[TPR < 64 ? 1 : TPR / 64][2][2];
     u32 slot = 0;
     const u32 t = threadIdx.x % TPR, groups = gridDim.x * (THREADS / TPR);
     const Columns<V, K, TPR> at(a.cols, t);
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR, GROUPS = THREADS / TPR;
-    __shared__ float ex[TPR / 64][2][2];
+    __shared__ float ex[TPR < 64 ? 1 : TPR / 64][2][2];
     __shared__ __attribute__((aligned(16))) float weight[K][TPR][V];
     u32 slot = 0;
     const u32 t = threadIdx.x % TPR, groups = gridDim.x * GROUPS;
@@ -331,23 +334,20 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(NormArgs a) {
     }
 }
 
-// dw[c], db[c] = the sums of all parts, always in the same order.  COLS columns per block, 1024 / COLS threads share a column's
-// parts: 64 columns read whole lines (512 parts of 8192 columns 6.7 us, with 16 11.8), 16 leave fewer loads that wait for one
-// another where there are few columns (14132 rows of 218, 1536 parts: forward and gradient 23.6 us, with 64 28.1).
-template <class TW, int COLS>
+// dw[c], db[c] = the sums of all parts, always in the same order.  64 columns per block, so that whole lines are read, and 16 threads
+// to share a column's parts: 512 parts of 8192 columns 6.7 us, bound by memory; 256 of 1280 3.5, by the loads' latency.
+template <class TW>
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restrict__ part, u32 parts, u32 cols, TW *dw, TW *db) {
-    __shared__ float join[16][COLS];
-    const u32 c = threadIdx.x % COLS, q = threadIdx.x / COLS;
-    const u64 col = (u64)blockIdx.x * COLS + c;
+    __shared__ float join[16][64];
+    const u32 c = threadIdx.x % 64, q = threadIdx.x / 64;
+    const u64 col = (u64)blockIdx.x * 64 + c;
     TW *out = blockIdx.y ? db : dw;
     if (!out) return;
     float s = 0.0f;
     if (col < cols)
 #pragma unroll 8
-        for (u32 p = q; p < parts; p += 1024 / COLS) s += part[((size_t)p * 2 + blockIdx.y) * cols + col];
-#pragma unroll
-    for (int o = COLS; o < 64; o <<= 1) s += __shfl_xor(s, o);
-    if ((threadIdx.x & 63) < COLS) join[threadIdx.x >> 6][c] = s;
+        for (u32 p = q; p < parts; p += 16) s += part[((size_t)p * 2 + blockIdx.y) * cols + col];
+    join[q][c] = s;
     __syncthreads();
     if (q == 0 && col < cols) {
         s = 0.0f;
@@ -358,10 +358,7 @@ __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restric
 }
 template <class TW>
 static void launch_parts(const float *part, u32 parts, u32 cols, void *dw, void *db, hipStream_t st) {
-    if (cols >= 4096)
-        hipLaunchKernelGGL((norm_parts_kernel<TW, 64>), dim3((cols + 63) / 64, 2), dim3(1024), 0, st, part, parts, cols, (TW *)dw, (TW *)db);
-    else
-        hipLaunchKernelGGL((norm_parts_kernel<TW, 16>), dim3((cols + 15) / 16, 2), dim3(1024), 0, st, part, parts, cols, (TW *)dw, (TW *)db);
+    hipLaunchKernelGGL((norm_parts_kernel<TW>), dim3((u32)(((u64)cols + 63) / 64), 2), dim3(1024), 0, st, part, parts, cols, (TW *)dw, (TW *)db);
 }
 
 // Threads per row and entries per thread: the smallest group whose registers hold the row at up to 32 entries a thread
@@ -369,24 +366,28 @@ static void launch_parts(const float *part, u32 parts, u32 cols, void *dw, void 
 // more exchanges and has fewer bytes under way.  us forward, gradient (bf16):
 //   16384 x 2048: 64 threads 25.2, 45.9; 256 threads 29.0, 60.2      8192 x 8192: 256 threads 45.4, 99.8; 1024 threads 79.7, 115
 //   32768 x 1536: 64 threads 35.7, 61.8; 256 threads 53.6, 88.8      64 x 2048: 3.9, 9.8 and 3.3, 7.9: not worth a second rule
-// 24 entries where they do rather than 32: 16384 x 1280 15.8, 31.6 (32: 17.2, 34.7), 4000 x 4800 f32 27.0, 51.0 (27.7, 60.2).
+// Rows of up to 256 leave most of a wave idle: 65000 x 64 bf16 16 threads 6.8, 14.5 (64: 17.6, 29.8), 56383 x 203 32 threads 11.4, 22.7
+// (64: 19.1, 33.0).  24 entries where they do rather than 32: 16384 x 1280 15.8, 31.6 (32: 17.2, 34.7), 4000 x 4800 f32 27.0, 51.0 (27.7, 60.2).
 struct NormShape {
     u32 tpr, e;
 };
 static NormShape norm_shape(u32 cols) {
     if (cols < 8) return {0, 0};
+    if (cols <= 16 * 8) return {16, 8};
+    if (cols <= 32 * 8) return {32, 8};
     if (cols <= 64 * 32) return {64, cols <= 64 * 8 ? 8u : cols <= 64 * 16 ? 16u : cols <= 64 * 24 ? 24u : 32u};
     if (cols <= 256 * 32) return {256, cols <= 256 * 16 ? 16u : cols <= 256 * 24 ? 24u : 32u};
     if (cols <= 1024 * 16) return {1024, 16};
     return {0, 0};
 }
 // Blocks: as many as the registers let run at once on 256 CUs, each with every so-manieth row.  Each block of the gradient leaves
-// one pair of column sums, so beyond one block for each CU its groups have four rows at least (us with a row each: 1000 x 5000 bf16
-// 25.1, 29.4; 4099 x 1280 f16 17.6, 18.5; 2000 x 768 f32 11.2, 13.8).
+// one pair of column sums, so it has fewer: two or three a CU (16384 x 4000 bf16 88.6 us, with four 98.5; 60000 x 300 33.1, with six
+// 36.9), and beyond one a CU its groups have four rows at least (1000 x 5000 bf16 23.7 us, with a row each 29.4; 4099 x 1280 f16 17.6,
+// 18.5; 2000 x 768 f32 11.4, 13.8).
 static u32 norm_blocks(u32 rows, const NormShape &s, bool grad) {
-    const u32 per = s.tpr == 64 ? 4 : 1, most = (rows + per - 1) / per;
+    const u32 per = s.tpr <= 64 ? 256 / s.tpr : 1, most = (rows + per - 1) / per;
     if (!grad) return std::min<u32>(most, 256 * (s.tpr == 1024 ? 1 : s.e == 32 ? 3 : s.e == 24 ? 4 : 6));
-    const u32 cu = s.tpr == 1024 ? 1 : s.e >= 24 ? 2 : s.e == 16 ? 4 : 6;
+    const u32 cu = s.tpr == 1024 ? 1 : s.e >= 16 ? 2 : 3;
     return std::min(most, std::max<u32>(256, std::min(256 * cu, rows / (4 * per))));
 }
 static u32 norm_grad_blocks(u32 rows, u32 cols) {
@@ -403,6 +404,8 @@ static void launch_norm(const NormArgs &a, hipStream_t st) {
         hipLaunchKernelGGL((norm_kernel<T, TW, TPR, E>), dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);         \
         return;                                                                                                           \
     }
+    CKKS_NORM(16, 8)
+    CKKS_NORM(32, 8)
     CKKS_NORM(64, 8)
     CKKS_NORM(64, 16)
     CKKS_NORM(64, 24)
@@ -423,6 +426,8 @@ static void launch_norm_grad(const NormArgs &a, u32 blocks, hipStream_t st) {
         hipLaunchKernelGGL((norm_grad_kernel<T, TW, TPR, E>), dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st, a);    \
         return;                                                                                                           \
     }
+    CKKS_NORM(16, 8)
+    CKKS_NORM(32, 8)
     CKKS_NORM(64, 8)
     CKKS_NORM(64, 16)
     CKKS_NORM(64, 24)

@@ -55,6 +55,15 @@ def test_against_64_bits(cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols", [8, 9, 15, 100, 127, 128, 129, 200, 255, 256, 257, 1536, 1537])
+def test_rows_that_share_a_wave(cols, dtype):
+    """Narrow rows, odd numbers of them, fewer and more than the blocks have at once."""
+    from paper_2604_09975_amd import clear as K
+    for rows in (2, 17, 4099):
+        check(K, *inputs(rows, cols, TYPES[dtype], cols + rows))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_many_rows_and_parameters_of_the_rows_type(dtype):
     from paper_2604_09975_amd import clear as K
     t = TYPES[dtype]

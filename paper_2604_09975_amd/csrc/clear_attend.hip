@@ -12,7 +12,7 @@
 // Either may split the keys over several blocks; a second kernel then joins the blocks' results in order.
 //
 // Measured (heads of 128, 32 query and 8 kv heads, 16 bits, unless said):
-//   prompts, 2 chunks of up to 4096 tokens over 12301 more keys, RW = 8: 1265 us, 1.04 PFLOP/s, where a library product of 8192^3
+//   prompts, 2 chunks of up to 4096 tokens over 12301 more keys, RW = 8: 1265 to 1300 us, 1.02 to 1.04 PFLOP/s, where a library product of 8192^3
 //     reaches 1.13; the matrix units are fed half the cycles and the softmax's arithmetic takes nearly as many, at a clock that
 //     the power limit holds down;
 //   64 single tokens over up to 8192 keys each, KW = 4: 225 us for 1.2 GB, 5.3 TB/s;

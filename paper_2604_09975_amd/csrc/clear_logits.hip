@@ -3,8 +3,8 @@
 // through the mask, and then writes the changed ones over it.  The tallies are whole numbers, and of several biases the largest
 // index counts: no order shows in a result.
 // Bound by memory where there is no history (256 x 131072 bf16 with a mask 29 us, 4.8 TB/s); with one by the chain of its lookups,
-// which a second block on the CU hides in part (the same with 4000 tokens a row 52 us, with up to 4000 and 100 biases 56), and by the launch for a
-// row (50257 f32, 5.5 us).  Measured and dropped: a launch for the masked copy and one that tallies a row's history by hashing
+// which a second block on the CU hides in part (the same with 4000 tokens a row 52 us, with up to 4000 and 100 biases 54 to 56), and by the launch for a
+// row (50257 f32, 5.4 us).  Measured and dropped: a launch for the masked copy and one that tallies a row's history by hashing
 // (64.9 us with 4000 tokens a row, 41.8 with 1000, where this takes 51.2 and 43.9; 256 x 131072 f32 110 and 71.6 against 75 and 60).
 #include <algorithm>
 

@@ -66,7 +66,7 @@ struct Columns {
 
 // TPR threads hold a row, E entries each: mean, then the sum of squares about it (two passes over registers: no cancellation), then
 // the scaled row.  Bound by memory: 16384 x 8192 bf16 in 92 us, 5.8 TB/s of the 4.9 that a large copy reaches (part of it lies in
-// the last cache); 4099 x 1280 f16 7.6 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
+// the last cache); 4099 x 1280 f16 7.4 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 
 // As norm_kernel with rows of x and dy.  The weight lies in LDS: registers hold the sums of the columns and the row that comes
 // next.  Bound by memory: 16384 x 8192 bf16 183 us, 4.6 TB/s with the sums that it writes (256 us with loads behind branches and
-// no row ahead); 4099 x 1280 f16 14.2 us, by the latency of the few rows that each group then has.
+// no row ahead); 4099 x 1280 f16 14.0 us, by the latency of the few rows that each group then has.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR, GROUPS = THREADS / TPR;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(1024) void norm_grad_wide_kernel(NormArgs a) {
 }
 
 // dw[c], db[c] = the sums of all parts, always in the same order.  64 columns per block, so that whole lines are read, and 16 threads
-// to share a column's parts: 512 parts of 8192 columns 6.7 us, bound by memory; 256 of 1280 3.5, by the loads' latency.
+// to share a column's parts: 512 parts of 8192 columns 6.7 us, bound by memory; 256 of 1280 3.8, by the loads' latency.
 template <class TW>
 __global__ __launch_bounds__(1024) void norm_parts_kernel(const float *__restrict__ part, u32 parts, u32 cols, TW *dw, TW *db) {
     __shared__ float join[16][64];

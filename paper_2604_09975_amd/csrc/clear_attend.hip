@@ -57,19 +57,27 @@ __device__ __forceinline__ f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
     for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
     return c;
 }
+// What the softmax's weights are held at, as powers of two: LIFT times exp2(score - maximum), where the maximum may lag by LAG.
+// In 16 bits a weight below 2^-14 loses bits and one below 2^-25 is gone, while the sum, in 32, counts it: beside one key that takes
+// most of a row, 1e5 others at 2^-24 of it came out as 0.0078 where they make up 0.0054.  F16 weights are therefore lifted
+// as far as the type goes, 2^15 with the lag (the lift cancels in out and is taken off lse): a weight keeps all its bits down to
+// 2^-25 of the largest and is gone from 2^-36.  BF16 has the range of 32 bits.
 template <class T>
 struct Frag;
 template <>
 struct Frag<float> {
     typedef f32x8 type;
+    static constexpr float LIFT = 0.0f, LAG = 8.0f;
 };
 template <>
 struct Frag<f16> {
     typedef f16x8 type;
+    static constexpr float LIFT = 11.0f, LAG = 4.0f;
 };
 template <>
 struct Frag<bf16> {
     typedef bf16x8 type;
+    static constexpr float LIFT = 0.0f, LAG = 8.0f;
 };
 
 template <class T>
@@ -200,6 +208,7 @@ template <class T, int DP, int RW, int KW, int TK, int OCC>
 __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a) {
     typedef AttendShape<T, DP, RW, KW, TK> Shape;
     typedef typename Frag<T>::type frag;
+    constexpr float LIFT = Frag<T>::LIFT, LAG = Frag<T>::LAG;
     constexpr int KS = Shape::KS, VS = Shape::VS, ROWS = 32 * RW, SUB = TK / 32, DT = DP / 32;
     constexpr int E = 16 / sizeof(T);                  // entries of a 16-byte piece
     constexpr int PIECES = DP / E;                     // pieces of a row
@@ -373,7 +382,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-    float m = -__builtin_inff(), l = 0.0f;  // maximum of the row's scores (kept up to 2^8, below), the lane's part of the sum
+    float m = -__builtin_inff(), l = 0.0f;  // maximum of the row's scores (it may lag, below), the lane's part of the sum
 
     f32x16 s[SUB];       // scores of a tile; accumulator i of a lane: key 8 (i / 4) + 4 half + i % 4 of its 32
     frag w[2 * SUB];     // weights, 16 keys each
@@ -424,9 +433,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
             for (int i = u ? 0 : 4; i < 16; ++i) tops[i % 4] = fmaxf(tops[i % 4], s[u][i]);
         const float top = other_half_max(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
-        // The maximum only has to keep exp2 in range: it moves when a score passes it by 8 powers of two, and then all
+        // The maximum only has to keep the weights in range: it moves when a score passes it by LAG powers of two, and then all
         // that was summed is scaled.
-        if (__any((top - m) * a.c > 8.0f)) {
+        if (__any((top - m) * a.c > LAG)) {
             const float mn = fmaxf(m, top);
             const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f((m - mn) * a.c);
             m = mn;
@@ -436,7 +445,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
         }
-        const float mc = m == -__builtin_inff() ? 0.0f : m * a.c;
+        const float mc = (m == -__builtin_inff() ? 0.0f : m * a.c) - LIFT;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
@@ -620,7 +629,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     if (KW == 1) {
         if (row0 + (lane & 31) >= r.rows) return;
         const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        const float lse2 = l > 0.0f || l != l ? __builtin_fmaf(m, a.c, __log2f(l)) : -__builtin_inff();
+        const float lse2 = l > 0.0f || l != l ? __builtin_fmaf(m, a.c, __log2f(l) - LIFT) : -__builtin_inff();
         const u64 at = (u64)(r.start + token) * a.heads + head;
         if (half == 0) {
             if (split_up)
@@ -691,7 +700,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
         }
         const bool some = sum > 0.0f || sum != sum;
         const float inv = some ? 1.0f / sum : 0.0f;
-        const float lse2 = some ? __builtin_fmaf(top, a.c, __log2f(sum)) : -__builtin_inff();
+        const float lse2 = some ? __builtin_fmaf(top, a.c, __log2f(sum) - LIFT) : -__builtin_inff();
         const u32 jrow = r.first_row + jr, jt = r.start + jrow / a.group, jh = kv_head * a.group + jrow % a.group;
         const u64 at = (u64)jt * a.heads + jh;
         Pack<float, 4> res = {{some ? acc.x * inv : 0.0f, some ? acc.y * inv : 0.0f, some ? acc.z * inv : 0.0f, some ? acc.w * inv : 0.0f}};

@@ -18,30 +18,37 @@ struct NormArgs {
     float eps;
 };
 
-// Sums of two values over the TPR threads of a group.  `slot` alternates between two halves of the exchange area, so one
+// Sums of two values (of p alone without BOTH) over the TPR threads of a group.  `slot` alternates between two halves of the exchange area, so one
 // barrier per call is enough: a wave can be at most one call ahead.
-template <int TPR>
+template <int TPR, bool BOTH = true>
 __device__ __forceinline__ void group_sum2(float &p, float &q, float (*ex)[2][2], u32 &slot) {
 #pragma unroll
     for (int o = TPR < 64 ? TPR / 2 : 32; o; o >>= 1) {
         p += __shfl_xor(p, o);
-        q += __shfl_xor(q, o);
+        if (BOTH) q += __shfl_xor(q, o);
     }
     if (TPR > 64) {
         const u32 wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
             ex[wave][slot][0] = p;
-            ex[wave][slot][1] = q;
+            if (BOTH) ex[wave][slot][1] = q;
         }
         __syncthreads();
-        p = q = 0.0f;
+        p = 0.0f;
+        if (BOTH) q = 0.0f;
 #pragma unroll
         for (int i = 0; i < TPR / 64; ++i) {
             p += ex[i][slot][0];
-            q += ex[i][slot][1];
+            if (BOTH) q += ex[i][slot][1];
         }
         slot ^= 1;
     }
+}
+
+// 1 / sqrt(variance + eps) from the mean square of differences whose own mean is `off`, small beside them or all there is of them.
+__device__ __forceinline__ float row_rstd(float square, float off, float eps) {
+    const float var = __builtin_fmaf(-off, off, square);
+    return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
 }
 
 // A thread's E entries of a row: chunks of 16 bytes, TPR chunks apart.  A chunk that would pass the end of the row is moved back
@@ -64,9 +71,11 @@ struct Columns {
     }
 };
 
-// TPR threads hold a row, E entries each: mean, then the sum of squares about it (two passes over registers: no cancellation), then
-// the scaled row.  Bound by memory: 16384 x 8192 bf16 in 92 us, 5.8 TB/s of the 4.9 that a large copy reaches (part of it lies in
-// the last cache); 4099 x 1280 f16 7.4 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
+// TPR threads hold a row, E entries each: a first mean, then the sums of the differences from it and of their squares, then the
+// scaled row.  The first mean is off by what its sum and 1/cols were rounded by, a few last places of the row's offset, which
+// rstd would multiply; the mean of the differences is that error, and is taken off them: 119 entries of 1e4 have no deviation.
+// Bound by memory: 16384 x 8192 bf16 in 92 us, 5.8 TB/s of the 4.9 that a large copy reaches (part of it lies in the last cache);
+// 4099 x 1280 f16 7.4 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
@@ -95,7 +104,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
     }
     const float inv = 1.0f / (float)a.cols;
     for (; row < a.rows; row += groups) {
-        float v[K][V], s = 0.0f, none = 0.0f;
+        float v[K][V], s = 0.0f, q = 0.0f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -112,29 +121,33 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 #pragma unroll
                 for (int i = 0; i < V; ++i) s += v[k][i];
         }
-        group_sum2<TPR>(s, none, ex, slot);
-        const float mean = s * inv;
-        float q = 0.0f;
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[k][i] -= mean;
+        group_sum2<TPR, false>(s, q, ex, slot);
+        const float first = s * inv;
+        s = q = 0.0f;
         if (at.ragged) {
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) q = __builtin_fmaf(i >= at.skip[k] ? v[k][i] : 0.0f, v[k][i], q);
+                for (int i = 0; i < V; ++i) {
+                    v[k][i] -= first;
+                    const float d = i >= at.skip[k] ? v[k][i] : 0.0f;
+                    s += d;
+                    q = __builtin_fmaf(d, v[k][i], q);
+                }
         } else {
 #pragma unroll
             for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int i = 0; i < V; ++i) q = __builtin_fmaf(v[k][i], v[k][i], q);
+                for (int i = 0; i < V; ++i) {
+                    v[k][i] -= first;
+                    s += v[k][i];
+                    q = __builtin_fmaf(v[k][i], v[k][i], q);
+                }
         }
-        none = 0.0f;
-        group_sum2<TPR>(q, none, ex, slot);
-        const float r = 1.0f / sqrtf(__builtin_fmaf(q, inv, a.eps));
+        group_sum2<TPR>(s, q, ex, slot);
+        const float off = s * inv, r = row_rstd(q * inv, off, a.eps), shift = -off * r;
         if (t == 0 && a.mean) {
-            a.mean[row] = mean;
+            a.mean[row] = first + off;
             a.rstd[row] = r;
         }
         T *y = (T *)a.y + (i64)row * a.ys;
@@ -142,7 +155,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
         for (int k = 0; k < K; ++k) {
             Pack<T, V> p;
 #pragma unroll
-            for (int i = 0; i < V; ++i) p.v[i] = (T)__builtin_fmaf(v[k][i] * r, w[k][i], b[k][i]);
+            for (int i = 0; i < V; ++i) p.v[i] = (T)__builtin_fmaf(__builtin_fmaf(v[k][i], r, shift), w[k][i], b[k][i]);
             if (at.skip[k] < V) store_pack<V>(y + at.col[k], p);
         }
     }
@@ -272,24 +285,25 @@ __global__ __launch_bounds__(1024) void norm_wide_kernel(NormArgs a) {
     for (u32 row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = (const T *)a.x + (i64)row * a.xs;
         T *y = (T *)a.y + (i64)row * a.ys;
-        float s = 0.0f, q = 0.0f, none = 0.0f;
+        float s = 0.0f, q = 0.0f;
         for (u64 c = threadIdx.x; c < a.cols; c += 1024) s += (float)x[c];
-        group_sum2<1024>(s, none, ex, slot);
-        const float mean = s * inv;
+        group_sum2<1024, false>(s, q, ex, slot);
+        const float first = s * inv;
+        s = q = 0.0f;
         for (u64 c = threadIdx.x; c < a.cols; c += 1024) {
-            const float d = (float)x[c] - mean;
+            const float d = (float)x[c] - first;
+            s += d;
             q = __builtin_fmaf(d, d, q);
         }
-        none = 0.0f;
-        group_sum2<1024>(q, none, ex, slot);
-        const float r = 1.0f / sqrtf(__builtin_fmaf(q, inv, a.eps));
+        group_sum2<1024>(s, q, ex, slot);
+        const float off = s * inv, r = row_rstd(q * inv, off, a.eps);
         if (threadIdx.x == 0 && a.mean) {
-            a.mean[row] = mean;
+            a.mean[row] = first + off;
             a.rstd[row] = r;
         }
         for (u64 c = threadIdx.x; c < a.cols; c += 1024) {
             const float w = a.w ? (float)((const TW *)a.w)[c] : 1.0f, b = a.b ? (float)((const TW *)a.b)[c] : 0.0f;
-            y[c] = (T)__builtin_fmaf(((float)x[c] - mean) * r, w, b);
+            y[c] = (T)__builtin_fmaf(((float)x[c] - first - off) * r, w, b);
         }
     }
 }

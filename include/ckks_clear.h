@@ -14,7 +14,7 @@
  *  - Lengths, page tables, token ids and positions are device data and are not read by the host.  A value that is out of
  *    range never makes a kernel touch memory outside the arrays described; what it does instead is said below.
  *  - Outputs may not overlap inputs unless said: CKKS_E_INVAL, nothing enqueued.  The test goes by the whole extent
- *    of an array, first to last element.
+ *    of an array, first to last element, unless said.
  */
 #ifndef CKKS_CLEAR_H
 #define CKKS_CLEAR_H
@@ -86,7 +86,8 @@ typedef struct {
  * d_cos / d_sin [n_pos][rot/2] (f32) at the token's position, or at d_positions[row] (int32 [n_tokens]) if that is given.
  * The rotation is computed in 32 bits and rounded once.  A position outside [0, n_pos) has no angle: the rotated
  * entries come out as NaN.  Tokens at a position below 0 and pages outside [0, n_pages) are not stored.
- * d_k, d_v: rows by strides {token, head}.  d_q may be NULL; d_q_out may be d_q with the same strides.  A row in no sequence has no
+ * d_k, d_v: rows by strides {token, head}.  d_q may be NULL; d_q_out may be d_q with the same strides, and then lie between the
+ * rows of the new keys and values (columns of one array) as long as it shares no entry with them.  A row in no sequence has no
  * position.  heads and kv_heads: at most 65536. */
 #define CKKS_CLEAR_INTERLEAVED 1u
 typedef struct {

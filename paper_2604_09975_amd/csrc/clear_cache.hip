@@ -190,14 +190,16 @@ extern "C" int ckks_clear_cache_append(const ckks_clear_append_t *p, void *strea
                           extent(b.d_page_table, 4, {{b.n_seq, b.table_stride}, {b.table_width, 1}}),
                           extent(p->d_q, e, {{heads ? b.n_tokens : 0, p->q_stride[0]}, {heads, p->q_stride[1]}, {g.head_dim, 1}})};
     const Extent places = extent(p->d_positions, 4, {{p->d_positions ? b.n_tokens : 0, 1}});
+    const auto runs = [&](const void *at, u32 n, const int64_t *st) { return Runs{at, g.head_dim * e, 2, {{b.n_tokens, st[0] * e}, {n, st[1] * e}}}; };
+    const Runs rows[3] = {runs(p->d_new_k, g.kv_heads, p->new_k_stride), runs(p->d_new_v, g.kv_heads, p->new_v_stride), runs(p->d_q_out, heads, p->q_out_stride)};
     const bool in_place = p->d_q == p->d_q_out && p->q_stride[0] == p->q_out_stride[0] && p->q_stride[1] == p->q_out_stride[1];
     bool bad = overlap(out[2], out[0]) || overlap(out[2], out[1]);  // keys and values may share one array, page by page
     for (int o = 0; o < 3; ++o) {
         bad |= overlap(out[o], places);
-        // the extents of new keys, values and queries interleave where they are columns of one array: q_out in place of q
-        // then meets k and v without sharing an entry
+        // the extents of new keys, values and queries interleave where they are columns of one array: with q_out in place of q
+        // keys and values are asked for entries that they share with it
         for (int i = 0; i < 8; ++i)
-            if (!(o == 2 && in_place && (i == 7 || i < 2))) bad |= overlap(out[o], in[i]);
+            if (overlap(out[o], in[i])) bad |= !(o == 2 && in_place) || (i < 2 ? share(rows[2], rows[i]) : i != 7);
     }
     if (bad) {
         set_error("%s: an output overlaps another array", who);

@@ -4,6 +4,7 @@
 
 #include "../../include/ckks_clear.h"
 #include "ckks_internal.h"
+#include "clear_extent.h"
 
 namespace ckks {
 
@@ -51,19 +52,6 @@ __device__ __forceinline__ void store_part(T *p, const Pack<T, N> &x, int n) {
 inline bool clear_dtype_ok(u32 d) { return d <= CKKS_CLEAR_BF16; }
 inline u32 clear_dtype_bytes(u32 d) { return d == CKKS_CLEAR_F32 ? 4 : 2; }
 
-// Bytes [lo, hi) that an array of rows touches: `n` counts and strides (in elements), outermost first.
-struct Extent {
-    uintptr_t lo, hi;
-};
-inline Extent extent(const void *p, u32 elem_bytes, std::initializer_list<std::pair<u64, i64>> dims) {
-    i64 lo = 0, hi = 0;
-    for (const auto &d : dims) {
-        if (!d.first) return {0, 0};
-        const i64 span = (i64)(d.first - 1) * d.second;
-        (span < 0 ? lo : hi) += span;
-    }
-    return {(uintptr_t)p + (uintptr_t)(lo * elem_bytes), (uintptr_t)p + (uintptr_t)((hi + 1) * elem_bytes)};
-}
 // What append and attend ask of the pages and the batch alike.
 inline int check_cache(const char *who, const ckks_clear_pages_t &g, const ckks_clear_batch_t &b) {
     if (!clear_dtype_ok(g.dtype) || !g.head_dim || g.head_dim % 8 || g.head_dim > 256 || !g.kv_heads || g.kv_heads > 1u << 16 || !g.page_size) {
@@ -89,7 +77,5 @@ inline int check_cache(const char *who, const ckks_clear_pages_t &g, const ckks_
     }
     return CKKS_OK;
 }
-
-inline bool overlap(const Extent &a, const Extent &b) { return a.lo < b.hi && b.lo < a.hi && a.lo != a.hi && b.lo != b.hi; }
 
 }  // namespace ckks

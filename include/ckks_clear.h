@@ -86,6 +86,7 @@ typedef struct {
  * d_cos / d_sin [n_pos][rot/2] (f32) at the token's position, or at d_positions[row] (int32 [n_tokens]) if that is given.
  * The rotation is computed in 32 bits and rounded once.  A position outside [0, n_pos) has no angle: the rotated
  * entries come out as NaN.  Tokens at a position below 0 and pages outside [0, n_pages) are not stored.
+ * Keys and values may lie in one array as long as they share no entry of it.
  * d_k, d_v: rows by strides {token, head}.  d_q may be NULL; d_q_out may be d_q with the same strides, and then lie between the
  * rows of the new keys and values (columns of one array) as long as it shares no entry with them.  A row in no sequence has no
  * position.  heads and kv_heads: at most 65536. */

@@ -193,7 +193,12 @@ extern "C" int ckks_clear_cache_append(const ckks_clear_append_t *p, void *strea
     const auto runs = [&](const void *at, u32 n, const int64_t *st) { return Runs{at, g.head_dim * e, 2, {{b.n_tokens, st[0] * e}, {n, st[1] * e}}}; };
     const Runs rows[3] = {runs(p->d_new_k, g.kv_heads, p->new_k_stride), runs(p->d_new_v, g.kv_heads, p->new_v_stride), runs(p->d_q_out, heads, p->q_out_stride)};
     const bool in_place = p->d_q == p->d_q_out && p->q_stride[0] == p->q_out_stride[0] && p->q_stride[1] == p->q_out_stride[1];
-    bool bad = overlap(out[2], out[0]) || overlap(out[2], out[1]);  // keys and values may share one array, page by page
+    const auto cells = [&](const void *at, const int64_t *st) {
+        return Runs{at, g.head_dim * e, 3, {{g.n_pages, st[0] * e}, {g.kv_heads, st[1] * e}, {g.page_size, st[2] * e}}};
+    };
+    bool bad = overlap(out[2], out[0]) || overlap(out[2], out[1]);
+    // keys and values may lie in one array, page by page, but not in the same places of it
+    if (overlap(out[0], out[1])) bad |= share(cells(g.d_k, g.k_stride), cells(g.d_v, g.v_stride));
     for (int o = 0; o < 3; ++o) {
         bad |= overlap(out[o], places);
         // the extents of new keys, values and queries interleave where they are columns of one array: with q_out in place of q

@@ -85,3 +85,12 @@ Q = dict(q=8 * P, q_out=8 * P)   # 4 heads of 64 in place, 16 bits
 ])
 def test_keys_and_values_that_share_entries_with_queries_in_place(bad):
     assert append(**bad) == -1 and "overlaps" in last()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(v=P), dict(v=P + 2 * 8), dict(v=P + 2 * 2048), dict(v=P + 2 * 1024),                     # the keys' places, some of them, the next page's
+    dict(ks0=4096, vs0=4096, v=P + 2 * 2040), dict(ks2=128, vs2=128, v=P + 2 * 60),               # beside the keys, but not quite
+    dict(v=P + 2 * 1024 * 5, vs0=1024, vs1=0),                                                    # other strides
+])
+def test_values_in_the_places_of_keys(bad):
+    assert append(**bad) == -1 and "overlaps" in last()

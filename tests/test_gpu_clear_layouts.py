@@ -47,3 +47,32 @@ def test_in_place_over_shared_entries_is_refused():
     for q, k, v in ((x[:, :H], x[:, :H], x[:, H:]), (x[:, :H], x[:, H:], x[:, :H]), (x[:, :H], x[:, 1:H + 1], x[:, H:]), (x[:, ::2], x[:, 2:6], x[:, 1::2])):
         with pytest.raises(B.CkksError, match="overlaps"):
             K.ckks_clear_cache_append(k, v, *c.args(), q=q, q_out=q)
+
+
+@pytest.mark.parametrize("order", ["page", "head", "row", "entry", "row heads"])
+def test_keys_and_values_of_one_array(order):
+    """Side by side in every order: page by page, head by head, row by row, entry by entry of a row."""
+    from paper_2604_09975_amd import clear as K
+    n = 6
+    shape = {"page": (n, 2, H, 16, D), "head": (n, H, 2, 16, D), "row": (n, H, 16, 2, D), "entry": (n, H, 16, 2 * D), "row heads": (n, 16, 2, H, D)}[order]
+    both = randn(gen(7), *shape, dtype=torch.float16)
+    kp, vp = {"page": lambda x: (x[:, 0], x[:, 1]), "head": lambda x: (x[:, :, 0], x[:, :, 1]), "row": lambda x: (x[..., 0, :], x[..., 1, :]),
+              "entry": lambda x: (x[..., :D], x[..., D:]), "row heads": lambda x: (x[:, :, 0].transpose(1, 2), x[:, :, 1].transpose(1, 2))}[order](both)
+    c = Cache([(T, 40), (1, 30)], H, H, D, 16, torch.float16, 8, spare=1)
+    assert c.k.shape == kp.shape
+    kp.copy_(c.k)
+    vp.copy_(c.v)
+    k, v = (randn(gen(s), T + 1, H, D, dtype=torch.float16) for s in (9, 10))
+    K.ckks_clear_cache_append(k, v, *c.args())
+    K.ckks_clear_cache_append(k, v, kp, vp, c.page_table, c.q_start, c.kv_len)
+    assert torch.equal(kp, c.k) and torch.equal(vp, c.v)
+    assert torch.equal(K.ckks_clear_attend(c.q, kp, vp, c.page_table, c.q_start, c.kv_len), K.ckks_clear_attend(c.q, *c.args()))
+
+
+def test_keys_in_the_places_of_values_are_refused():
+    from paper_2604_09975_amd import binding as B
+    from paper_2604_09975_amd import clear as K
+    c = Cache([(T, T)], H, H, D, 16, torch.float16, 11)
+    k = randn(gen(12), T, H, D, dtype=torch.float16)
+    with pytest.raises(B.CkksError, match="overlaps"):
+        K.ckks_clear_cache_append(k, k, c.k, c.k, c.page_table, c.q_start, c.kv_len)

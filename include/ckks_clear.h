@@ -14,7 +14,7 @@
  *  - Lengths, page tables, token ids and positions are device data and are not read by the host.  A value that is out of
  *    range never makes a kernel touch memory outside the arrays described; what it does instead is said below.
  *  - Outputs may not overlap inputs unless said: CKKS_E_INVAL, nothing enqueued.  The test goes by the whole extent
- *    of an array, first to last element, unless said.
+ *    of an array, first to last element, unless said.  Neither may the rows of one output overlap one another.
  */
 #ifndef CKKS_CLEAR_H
 #define CKKS_CLEAR_H

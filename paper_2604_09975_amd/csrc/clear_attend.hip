@@ -984,6 +984,10 @@ int ckks_clear_attend(const ckks_clear_attend_t *p, void *stream) {
         set_error("%s: an output overlaps another array", who);
         return CKKS_E_INVAL;
     }
+    if (share_within({p->d_out, g.head_dim * e, 2, {{b.n_tokens, p->out_stride[0] * e}, {p->heads, p->out_stride[1] * e}}})) {
+        set_error("%s: rows of the output overlap", who);
+        return CKKS_E_INVAL;
+    }
     AttendArgs a{};
     a.q = p->d_q, a.k = g.d_k, a.v = g.d_v, a.out = p->d_out, a.lse = p->d_lse;
     a.part_lse = (float *)p->d_work;

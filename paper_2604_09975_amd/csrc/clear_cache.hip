@@ -198,7 +198,8 @@ extern "C" int ckks_clear_cache_append(const ckks_clear_append_t *p, void *strea
     };
     bool bad = overlap(out[2], out[0]) || overlap(out[2], out[1]);
     // keys and values may lie in one array, page by page, but not in the same places of it
-    if (overlap(out[0], out[1])) bad |= share(cells(g.d_k, g.k_stride), cells(g.d_v, g.v_stride));
+    const Runs keys = cells(g.d_k, g.k_stride), values = cells(g.d_v, g.v_stride);
+    if (overlap(out[0], out[1])) bad |= share(keys, values);
     for (int o = 0; o < 3; ++o) {
         bad |= overlap(out[o], places);
         // the extents of new keys, values and queries interleave where they are columns of one array: with q_out in place of q
@@ -208,6 +209,10 @@ extern "C" int ckks_clear_cache_append(const ckks_clear_append_t *p, void *strea
     }
     if (bad) {
         set_error("%s: an output overlaps another array", who);
+        return CKKS_E_INVAL;
+    }
+    if (share_within(keys) || share_within(values) || (heads && share_within(rows[2]))) {
+        set_error("%s: rows of an output overlap", who);
         return CKKS_E_INVAL;
     }
     AppendArgs a{};

@@ -84,4 +84,35 @@ inline bool share(const Runs &a, const Runs &b) {
     return reaches((int64_t)((uintptr_t)a.at - (uintptr_t)b.at), a.run, s, n);
 }
 
+// Two runs of one array share a byte.
+inline bool share_within(const Runs &a) {
+    Step s[3];
+    // nested arrays, and those are nearly all, have each stride at least as wide as all that lies within it
+    int n = 0;
+    for (int k = 0; k < a.dims; ++k) {
+        if (!a.dim[k].n) return false;
+        if (a.dim[k].n == 1) continue;
+        s[n++] = {0, a.dim[k].n - 1, a.dim[k].stride < 0 ? -a.dim[k].stride : a.dim[k].stride};
+        for (int j = n - 1; j && s[j].stride < s[j - 1].stride; --j) std::swap(s[j], s[j - 1]);
+    }
+    int64_t span = a.run;
+    bool nested = true;
+    Step all[3];
+    for (int k = 0; k < n; ++k) {
+        nested &= s[k].stride >= span;
+        span += s[k].hi * s[k].stride;
+        all[k] = s[k];
+    }
+    if (nested) return false;
+    // the first index in which the two runs differ, the others either way
+    const int dims = n;
+    for (int lead = 0; lead < dims; ++lead) {
+        n = 0;
+        s[n++] = {1, all[lead].hi, all[lead].stride};
+        for (int k = lead + 1; k < dims; ++k) s[n++] = {-all[k].hi, all[k].hi, all[k].stride};
+        if (reaches(0, a.run, s, n)) return true;
+    }
+    return false;
+}
+
 }  // namespace ckks

@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from tests.test_clear_abi import P, append, last
+from tests.test_clear_abi import P, append, attend, last
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2604_09975_amd", "csrc")
 
@@ -59,6 +59,18 @@ def test_shared_entries_are_found_exactly(tmp_path):
     assert 1000 < sum(want) < 5000 and [g == "1" for g in got] == want
 
 
+def test_arrays_that_meet_themselves_are_found_exactly(tmp_path):
+    rng, asked, want = random.Random(2), [], []
+    for _ in range(6000):
+        n, run = rng.choice((2, 3)), rng.randint(1, 9)
+        a = layout(rng, n)
+        asked.append([1000, run, n] + [x for d in a for x in d])
+        all_of_it = cells(1000, run, a)
+        want.append(len(set(all_of_it)) < len(all_of_it))
+    got = ask(tmp_path, READ + 'int main() { Runs a; while (read(a)) puts(share_within(a) ? "1" : "0"); }', asked)
+    assert 1000 < sum(want) < 5000 and [g == "1" for g in got] == want
+
+
 def test_layouts_of_use_are_settled_quickly(tmp_path):
     """Queries beside keys of 10^6 tokens: columns of one array, heads side by side in either order, a head's query, key and value
     together; and the same with one entry shared.  Nothing here may run out of tries."""
@@ -94,3 +106,15 @@ def test_keys_and_values_that_share_entries_with_queries_in_place(bad):
 ])
 def test_values_in_the_places_of_keys(bad):
     assert append(**bad) == -1 and "overlaps" in last()
+
+
+@pytest.mark.parametrize("bad", [dict(o0=0), dict(o1=0), dict(o0=192), dict(o1=63), dict(o0=64, o1=128), dict(o0=200, o1=64), dict(o0=-255)])
+def test_rows_of_an_output_that_overlap(bad):
+    """(5 tokens of 4 heads of 64)"""
+    for call in (append, attend):
+        assert call(**bad) == -1 and "overlap" in last()
+
+
+@pytest.mark.parametrize("bad", [dict(ks0=0), dict(ks1=0), dict(vs1=0), dict(ks2=0), dict(vs2=63), dict(ks0=1984), dict(vs1=1000), dict(ks1=32, ks2=64)])
+def test_pages_that_overlap_are_not_written(bad):
+    assert append(**bad) == -1 and "overlap" in last()

@@ -76,3 +76,31 @@ def test_keys_in_the_places_of_values_are_refused():
     k = randn(gen(12), T, H, D, dtype=torch.float16)
     with pytest.raises(B.CkksError, match="overlaps"):
         K.ckks_clear_cache_append(k, k, c.k, c.k, c.page_table, c.q_start, c.kv_len)
+
+
+def test_rows_of_an_output_that_overlap_are_refused():
+    from paper_2604_09975_amd import binding as B
+    from paper_2604_09975_amd import clear as K
+    c = Cache([(T, 40)], H, H, D, 16, torch.float16, 13)
+    k = randn(gen(14), T, H, D, dtype=torch.float16)
+    one = torch.empty(1, H, D, dtype=torch.float16, device="cuda")
+    for out in (one.expand(T, H, D), torch.empty(T, 1, D, dtype=torch.float16, device="cuda").expand(T, H, D)):
+        with pytest.raises(B.CkksError, match="overlap"):
+            K.ckks_clear_attend(c.q, *c.args(), out=out)
+        with pytest.raises(B.CkksError, match="overlap"):
+            K.ckks_clear_cache_append(k, k, *c.args(), q=c.q, q_out=out)
+    shared = c.k[:1].expand(c.k.shape)
+    with pytest.raises(B.CkksError, match="overlap"):
+        K.ckks_clear_cache_append(k, k, shared, c.v, c.page_table, c.q_start, c.kv_len)
+    assert torch.isfinite(K.ckks_clear_attend(c.q, shared, c.v, c.page_table, c.q_start, c.kv_len)).all()   # reading them is fine
+
+
+def test_outputs_that_interleave_without_overlapping():
+    """Rows of one output between one another, head by head or token by token, no stride as wide as all that lies within it."""
+    from paper_2604_09975_amd import clear as K
+    c = Cache([(2, 40)], 3, 3, D, 16, torch.float16, 15)
+    want = K.ckks_clear_attend(c.q, *c.args())
+    room = torch.zeros(8 * D, dtype=torch.float16, device="cuda")
+    out = room.as_strided((2, 3, D), (3 * D, 2 * D, 1))     # rows at 0, 2, 4 and 3, 5, 7
+    K.ckks_clear_attend(c.q, *c.args(), out=out)
+    assert torch.equal(out, want) and not room[D:2 * D].any() and not room[6 * D:7 * D].any()

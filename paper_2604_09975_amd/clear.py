@@ -4,12 +4,17 @@ Argument marshalling only, as in `binding`: every function has the name of the C
 the current HIP device and enqueues on torch's current stream.  Rows may be strided; their last dimension is contiguous.
 Types are float32, float16 and bfloat16.  Workspaces come from torch's allocator, on the stream of the call.
 
+None of the calls is recorded by autograd (a layer norm's gradient is a call of its own): a tensor that requires a gradient is
+refused while gradients are recorded.  Tensors that a call writes in place count as modified, so a backward pass that
+needs their old values notices.
+
 A call's kernels can take less time than its marshalling (one token: 4 to 7 us), so the argument struct is packed in one go
 and each tensor is asked for as little as its check needs.
 """
 import struct
 
 import torch
+from torch.autograd.graph import increment_version as _written
 
 from .binding import C, _check, _raw_stream, _stream, lib
 
@@ -43,9 +48,17 @@ def _on(dev):
     return _raw_stream(dev) if _raw_stream is not None else _stream()
 
 
+def _refuse(what):
+    """For a tensor that requires a gradient: it would be lost without a word."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, which this call does not record: detach it, or call under torch.no_grad()")
+
+
 def _ptr(t, dtype, dev, what):
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
         raise TypeError(f"{what}: expected a {dtype} tensor on device {dev}")
+    if t.requires_grad:
+        _refuse(what)
     return t.data_ptr()
 
 
@@ -55,6 +68,8 @@ def _vec(t, dtype, n, dev, what):
         return 0
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
         raise TypeError(f"{what}: expected a {dtype} tensor on device {dev}")
+    if t.requires_grad:
+        _refuse(what)
     if t.dim() != 1 or (n is not None and t.numel() != n) or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous vector" + (f" of {n}" if n is not None else ""))
     return t.data_ptr()
@@ -101,6 +116,7 @@ def ckks_clear_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stats=T
             wt = bt
         elif wt != bt:
             raise TypeError("weight and bias must be of one type")
+    given = out
     if out is None:
         out = torch.empty_like(x, memory_format=_rowwise)
         py, ys = out.data_ptr(), cols
@@ -118,6 +134,8 @@ def ckks_clear_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stats=T
     rc = _norm(_NORM(px, pw, pb, py, pm, pr, xs, ys, rows, cols, code, wt, eps, 0), _on(dev))
     if rc:
         _check(rc)
+    if given is not None:
+        _written(given)
     return out, mean, rstd
 
 
@@ -136,6 +154,7 @@ def ckks_clear_layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, params=T
     wt = pw = 0
     if weight is not None:
         wt, pw = _param(weight, dtype, cols, dev, "weight")
+    given = dx
     if dx is None:
         dx = torch.empty_like(x, memory_format=_rowwise)
         pdx, dxs = dx.data_ptr(), cols
@@ -157,6 +176,8 @@ def ckks_clear_layer_norm_grad(dy, x, mean, rstd, weight=None, dx=None, params=T
                                _rows(dy, "dy")[2], xs, dxs, rows, cols, code, wt), _on(dev))
     if rc:
         _check(rc)
+    if given is not None:
+        _written(given)
     return dx, dw, db
 
 
@@ -164,6 +185,8 @@ def _heads(t, dtype, n, dim, dev, what):
     """Pointer, heads and strides {token, head} of [n][heads][dim]."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != dev:
         raise TypeError(f"{what}: expected a {dtype} tensor on device {dev}")
+    if t.requires_grad:
+        _refuse(what)
     if t.dim() != 3:
         raise ValueError(f"{what} must be [{n}][heads][{dim}]")
     rows, heads, width = t.shape
@@ -230,6 +253,7 @@ def ckks_clear_cache_append(k, v, k_pages, v_pages, page_table, q_start, kv_len,
                          heads, rot, n_pos, 1 if interleaved else 0), _on(dev))
     if rc:
         _check(rc)
+    _written((k_pages, v_pages) if q is None else (k_pages, v_pages, q_out))
     return q_out
 
 
@@ -242,6 +266,7 @@ def ckks_clear_attend(q, k_pages, v_pages, page_table, q_start, kv_len, scale=No
     if dim != cache[11]:
         raise ValueError(f"q must be [{n}][heads][{cache[11]}]")
     pq, heads, q0, q1 = _heads(q, dtype, n, dim, dev, "q")
+    given = tuple(t for t in (out, lse) if t is not None)
     if out is None:
         out = torch.empty_like(q, memory_format=_rowwise)
         po, o0, o1 = out.data_ptr(), heads * dim, dim
@@ -265,6 +290,8 @@ def ckks_clear_attend(q, k_pages, v_pages, page_table, q_start, kv_len, scale=No
     rc = _attend(args, _on(dev))
     if rc:
         _check(rc)
+    if given:
+        _written(given)
     return out
 
 
@@ -274,6 +301,7 @@ def ckks_clear_logits(logits, out=None, tokens=None, token_start=None, n_prompt=
     dev, code, dtype = _device(), _type(logits, "logits"), logits.dtype
     pl = _ptr(logits, dtype, dev, "logits")
     rows, vocab, ls = _rows(logits, "logits")
+    given = out
     if out is None:
         out = torch.empty_like(logits, memory_format=_rowwise)
         po, os, oc = out.data_ptr(), vocab, code
@@ -298,4 +326,6 @@ def ckks_clear_logits(logits, out=None, tokens=None, token_start=None, n_prompt=
                 _vec(bias, _f32, n_biases, dev, "bias"), pm, ls, os, ms, rows, vocab, n_tokens, n_biases, code, oc), _on(dev))
     if rc:
         _check(rc)
+    if given is not None:
+        _written(given)
     return out

@@ -238,14 +238,15 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     const bool idle = row0 >= r.rows;                  // no row of this wave exists
     const u32 row = min(row0 + (lane & 31), r.rows - 1), token = row / a.group, head = kv_head * a.group + row % a.group;
     const int pos = max(r.t0 + (int)token, -1);
-    const int hi = a.causal ? min(r.kv, pos + 1) : r.kv, lo = a.window ? pos - a.window + 1 : 0;  // keys lo <= j < hi are seen
+    // keys lo <= j < hi are seen, and none of these bounds is below 0: their differences with a key's place stay in 32 bits
+    const int hi = a.causal ? min(r.kv, pos + 1) : r.kv, lo = a.window ? max(pos - a.window + 1, 0) : 0;
     // bounds over the wave's rows: keys that all of them see, keys that any of them sees
     const int p_first = row_pos(a, r, min(row0, r.rows - 1)), p_last = row_pos(a, r, min(row0 + 31, r.rows - 1));
     const int all_hi = a.causal ? min(r.kv, p_first + 1) : r.kv, any_hi = a.causal ? min(r.kv, p_last + 1) : r.kv;
     // ... of the block's rows
     const int block_hi = a.causal ? min(r.kv, row_pos(a, r, r.first_row) + 1) : r.kv,
-              block_lo = a.window ? row_pos(a, r, min(r.first_row + ROWS, r.rows) - 1) - a.window + 1 : 0;
-    const int all_lo = a.window ? p_last - a.window + 1 : 0, any_lo = a.window ? p_first - a.window + 1 : 0;
+              block_lo = a.window ? max(row_pos(a, r, min(r.first_row + ROWS, r.rows) - 1) - a.window + 1, 0) : 0;
+    const int all_lo = a.window ? max(p_last - a.window + 1, 0) : 0, any_lo = a.window ? max(p_first - a.window + 1, 0) : 0;
 
     frag qf[DP / 16];
     {
@@ -366,11 +367,11 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     u32 odd = 0;
     auto partial = [&](u32 tile) {
         const int j0 = (int)((r.tile0 + tile) * TK);
-        return j0 + TK > block_hi || j0 < block_lo;
+        return block_hi - j0 < TK || j0 < block_lo;
     };
     auto put_v = [&](u32 tile, T *buf) {
         blank(vr, v_none);
-        if (partial(tile) && tile < last)
+        if (tile < last && partial(tile))
 #pragma unroll
             for (int p = 0; p < PASSES; ++p) vr[p] = finite_part<T>(vr[p], odd);
 #pragma unroll
@@ -389,11 +390,11 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(AttendArgs a)
     // whether any row of the wave sees the tile, and whether some row does not see all of it
     auto seen = [&](u32 tile) {
         const int j0 = (int)((r.tile0 + tile) * TK);
-        return !idle && j0 < any_hi && j0 + TK > any_lo;
+        return !idle && j0 < any_hi && any_lo - j0 < TK;
     };
     auto masked = [&](u32 tile) {
         const int j0 = (int)((r.tile0 + tile) * TK);
-        return j0 + TK > all_hi || j0 < all_lo;
+        return all_hi - j0 < TK || j0 < all_lo;
     };
     auto see_lo = [&](u32 tile) { return lo - (int)((r.tile0 + tile) * TK) - 4 * (int)half; };
     auto see_hi = [&](u32 tile) { return hi - (int)((r.tile0 + tile) * TK) - 4 * (int)half; };

@@ -81,6 +81,8 @@ class Block:
     def chunk(self, tokens):
         """Up to SEGMENT tokens through the block: the rows before the last layer norm."""
         n = len(tokens)
+        if self.length + n > self.page_table.shape[1] * PAGE:
+            raise ValueError(f"{self.length + n} tokens in a cache of {self.page_table.shape[1] * PAGE}")
         self.length += n
         batch = (self.page_table, torch.tensor([0, n], dtype=torch.int32, device="cuda"),
                  torch.tensor([self.length], dtype=torch.int32, device="cuda"))

@@ -111,8 +111,11 @@ int ckks_clear_cache_append(const ckks_clear_append_t *a, void *stream);
  * does not see do not reach its result, whatever they hold.  A page outside [0, n_pages) reads as zeros.  scale > 0 and finite,
  * scores scale q.k and their multiples by log2(e) within the range of 32 bits.  Rows of q in no sequence are not written.
  * heads: a multiple of kv_heads, at most 65536, n_tokens * heads / kv_heads below 2^31.
- * With 16-bit types the softmax's weights are rounded to that type before they meet the values (F16: with its 11 bits
- * down to 2^-25 of the row's largest so far, to steps of 2^-35 of that below); all sums are 32-bit.  d_q, d_out: [n_tokens][heads][head_dim] by strides {token, head}; d_lse f32 [n_tokens][heads] or NULL.
+ * All sums are 32-bit.  With 16-bit types a weight of the softmax meets the values as a high and a low number of that type for
+ * single tokens and short chunks: only the result is rounded to the type.  For chunks whose products fill the device, by the
+ * measured costs of either way, it is rounded to the type: F16 with its 11 bits down to 2^-25 of the row's largest so far, to steps
+ * of 2^-35 of that below.
+ * d_q, d_out: [n_tokens][heads][head_dim] by strides {token, head}; d_lse f32 [n_tokens][heads] or NULL.
  * d_work: at least ckks_clear_attend_work_bytes bytes, 16-byte aligned, contents free (NULL if that is 0). */
 #define CKKS_CLEAR_CAUSAL 1u
 typedef struct {

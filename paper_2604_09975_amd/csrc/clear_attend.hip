@@ -12,12 +12,14 @@
 // Either may split the keys over several blocks; a second kernel then joins the blocks' results in order.
 //
 // Measured (heads of 128, 32 query and 8 kv heads, 16 bits, unless said):
-//   prompts, 2 chunks of up to 4096 tokens over 12301 more keys, RW = 8: 1265 to 1300 us, 1.02 to 1.04 PFLOP/s, where a library product of 8192^3
+//   prompts, 2 chunks of up to 4096 tokens over 12301 more keys, RW = 8: 1265 to 1315 us, 1.00 to 1.04 PFLOP/s, where a library product of 8192^3
 //     reaches 1.13; the matrix units are fed half the cycles and the softmax's arithmetic takes nearly as many, at a clock that
 //     the power limit holds down;
 //   64 single tokens over up to 8192 keys each, KW = 4: 225 us for 1.2 GB, 5.3 TB/s;
-//   1 token over 131002 keys, 16 and 2 heads, KW = 4, split: 26 us and 5 us to join (134 MB, 27 us at a copy's rate);
-//   1 token over 128 keys, 12 heads of 64: 6.4 us; 128 tokens of 32 bits: 10.4 us: the chain of lookup, load, product, join.
+//   1 token over 131002 keys, 16 and 2 heads, KW = 4, split: 26 to 30 us and 5 us to join (134 MB, 27 us at a copy's rate);
+//   1 token over 128 keys, 12 heads of 64: 6.9 us; 128 tokens of 32 bits: 10.7 us: the chain of lookup, load, product, join.
+//   Heads of 136 to 256 do not fit the registers: 172 of a lane lie in scratch with KW = 4 (64 tokens over 8192 keys, 8 heads of 256, bf16
+//     1.5 ms, 2.9 TB/s; one token 41 us), 38 with RW = 4 in 32 bits (88 TFLOP/s); RW = 4 in 16 bits reaches 590 TFLOP/s.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -846,7 +848,8 @@ constexpr AttendForm FORMS_128[] = {{1, 32, 32, 128, 6, 1.7f, 3.1f, 2}, {4, 128,
 constexpr AttendForm FORMS_256[] = {{1, 32, 32, 128, 8, 4, 4, 1}, {4, 128, 32, 32, 10, 2.2f, 2.2f, 1}};
 // 32-bit products are slow enough for each wave to read its keys by itself: with rows of 64 the form of shared tiles gains nothing
 // (32 heads, 2 x 1024 tokens over 3024 keys: 439 us, apart 447); with rows of 128, where only one block of waves apart fits a CU,
-// two with shared tiles do (963 -> 802 us).  Rows of 256 fit no other way.
+// two with shared tiles do (963 -> 802 us).  Rows of 256 fit no other way.  The full costs of 16-bit single tokens are those with low parts of
+// their weights (heads of 64 1.6, of 128 2.8 without).
 constexpr AttendForm FORMS_F32_64[] = {{1, 32, 32, 128, 6, 4, 4, 1}};
 constexpr AttendForm FORMS_F32_128[] = {{1, 32, 32, 128, 6, 8, 8, 1}, {4, 128, 32, 32, 10, 4.9f, 8.4f, 2}};
 constexpr AttendForm FORMS_F32_256[] = {{4, 128, 32, 32, 10, 14, 14, 1}};

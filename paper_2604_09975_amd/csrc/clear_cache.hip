@@ -1,7 +1,7 @@
 // New keys and values into their pages, keys and queries rotated on the way.  Every array is read and written once: bound by
 // memory, by the launch for a few tokens.  A thread moves V entries (rotated by halves: V of each half), a head's threads lie side
 // by side, and all three arrays are moved by one launch.  About 23000 tokens of 32 query and 8 kv heads of 128, bf16, rotated:
-// 568 MB in 116 to 123 us, 4.6 to 4.9 TB/s, what a large copy reaches; 32 single tokens of 12 heads 3.7 us.
+// 568 MB in 116 to 125 us, 4.5 to 4.9 TB/s, what a large copy reaches (pairs side by side 139); 32 single tokens of 12 heads 3.7 us.
 #include <algorithm>
 #include <numeric>
 

@@ -74,8 +74,8 @@ struct Columns {
 // TPR threads hold a row, E entries each: a first mean, then the sums of the differences from it and of their squares, then the
 // scaled row.  The first mean is off by what its sum and 1/cols were rounded by, a few last places of the row's offset, which
 // rstd would multiply; the mean of the differences is that error, and is taken off them: 119 entries of 1e4 have no deviation.
-// Bound by memory: 16384 x 8192 bf16 in 92 us, 5.8 TB/s of the 4.9 that a large copy reaches (part of it lies in the last cache);
-// 4099 x 1280 f16 7.4 us; 128 x 768 f32 3.6 us, a launch.  Weight and bias stay in registers over a block's rows.
+// Bound by memory: 16384 x 8192 bf16 in 93 us, 5.8 TB/s of the 4.9 that a large copy reaches (part of it lies in the last cache);
+// 4099 x 1280 f16 7.9 us; 128 x 768 f32 3.7 us, a launch.  Weight and bias stay in registers over a block's rows.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR;
@@ -163,7 +163,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormArgs a)
 
 // As norm_kernel with rows of x and dy.  The weight lies in LDS: registers hold the sums of the columns and the row that comes
 // next.  Bound by memory: 16384 x 8192 bf16 183 us, 4.6 TB/s with the sums that it writes (256 us with loads behind branches and
-// no row ahead); 4099 x 1280 f16 14.0 us, by the latency of the few rows that each group then has.
+// no row ahead); 4099 x 1280 f16 14.0 us, by the latency of four to five rows one after the other in each group, one wave on a SIMD.
+// f32 rows of 8193 to 16384 leave 31 registers of a thread in scratch: 4096 x 12000 173 us with the second kernel, 120 at a copy's rate.
 template <class T, class TW, int TPR, int E>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormArgs a) {
     constexpr int V = 16 / sizeof(T), K = E / V, THREADS = TPR < 256 ? 256 : TPR, GROUPS = THREADS / TPR;
@@ -276,7 +277,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_grad_kernel(NormAr
 }
 
 // Rows wider than the registers of a block, or shorter than an access: the same sums in loops over the row, which comes from the
-// caches again (4096 x 16400 bf16: 198 us, gradient 337; in registers 4096 x 16384 takes 49 and 102).
+// caches again, an entry at a time: 4096 x 16400 bf16 164 us, gradient 267, where 4096 x 16384 in registers takes 54 and 102; 65000 x 5
+// 390 and 490.
 template <class T, class TW>
 __global__ __launch_bounds__(1024) void norm_wide_kernel(NormArgs a) {
     __shared__ float ex[16][2][2];
@@ -377,11 +379,11 @@ static void launch_parts(const float *part, u32 parts, u32 cols, void *dw, void 
 
 // Threads per row and entries per thread: the smallest group whose registers hold the row at up to 32 entries a thread
 // (16 where 1024 threads share the register file).  0: none does, or the row is shorter than an access.  A larger group waits for
-// more exchanges and has fewer bytes under way.  us forward, gradient (bf16):
-//   16384 x 2048: 64 threads 25.2, 45.9; 256 threads 29.0, 60.2      8192 x 8192: 256 threads 45.4, 99.8; 1024 threads 79.7, 115
-//   32768 x 1536: 64 threads 35.7, 61.8; 256 threads 53.6, 88.8      64 x 2048: 3.9, 9.8 and 3.3, 7.9: not worth a second rule
-// Rows of up to 256 leave most of a wave idle: 65000 x 64 bf16 16 threads 6.8, 14.5 (64: 17.6, 29.8), 56383 x 203 32 threads 11.4, 22.7
-// (64: 19.1, 33.0).  24 entries where they do rather than 32: 16384 x 1280 15.8, 31.6 (32: 17.2, 34.7), 4000 x 4800 f32 27.0, 51.0 (27.7, 60.2).
+// more exchanges and has fewer bytes under way.  us forward (calls back to back in a graph), gradient (bf16):
+//   16384 x 2048: 64 threads 27.0, 45.9; 256 threads 33.6, 60.2      8192 x 8192: 256 threads 51.8, 99.8; 1024 threads 91.6, 115
+//   32768 x 1536: 64 threads 40.2, 61.8; 256 threads 58.8, 88.8      64 x 2048: 3.4, 9.8 and 3.1, 7.9: not worth a second rule
+// Rows of up to 256 leave most of a wave idle: 65000 x 64 bf16 16 threads 7.1, 14.5 (64: 20.7, 29.8), 56383 x 203 32 threads 11.8, 22.7
+// (64: 19.7, 33.0).  24 entries where they do rather than 32: 16384 x 1280 15.3, 31.6 (32: 17.1, 34.7), 4000 x 4800 f32 33.2, 51.0 (36.0, 60.2).
 struct NormShape {
     u32 tpr, e;
 };

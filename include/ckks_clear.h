@@ -1,7 +1,7 @@
 /*
  * The key holder's steps in the clear, on the device: what a transformer block computes on decrypted activations
  * between two encrypted projections (ckks.h).  Layer norm with its gradient, the key / value cache with the attention
- * over it, and the rules on logits before the next token is chosen.
+ * over it, in the activations' type or in 8 bits, the rules on logits and the draw of the next token.
  *
  * Conventions are those of ckks.h: 0 or a negative CKKS_E_* code with ckks_last_error(), device pointers carry "d_",
  * `stream` is a hipStream_t, calls enqueue and return, nothing is allocated and nothing is kept between calls, so they
@@ -158,6 +158,99 @@ typedef struct {
     uint32_t rows, vocab, n_tokens, n_biases, dtype, out_dtype;
 } ckks_clear_logits_t;
 int ckks_clear_logits(const ckks_clear_logits_t *a, void *stream);
+
+/* ---- key / value cache of 8 bits ------------------------------------------
+ * Pages whose entries are a byte each, a code, and whose rows have one byte more for each 32 entries of a head (the
+ * last block of a head may be shorter): the block's power of two.  An entry stands for code * 2^(power - 127), and the whole block for
+ * not-a-number where the power is 255.  Formats: CKKS_CLEAR_E4M3 (sign, 4 bits of exponent, 3 of mantissa, largest 448, no infinity,
+ * 0x7f and 0xff not-a-number), CKKS_CLEAR_I8 (two's complement).
+ * d_k, d_v [n_pages][kv_heads][page_size][head_dim] bytes and d_k_power, d_v_power [n_pages][kv_heads][page_size][ceil(head_dim / 32)]
+ * bytes, each by its strides {page, head, token}; limits, addressing of the batch and what values out of range do are those of
+ * ckks_clear_pages_t.  dtype: the type of queries, new rows and results. */
+#define CKKS_CLEAR_E4M3 16u
+#define CKKS_CLEAR_I8 17u
+typedef struct {
+    uint8_t *d_k, *d_v, *d_k_power, *d_v_power;
+    int64_t k_stride[3], v_stride[3], k_power_stride[3], v_power_stride[3];
+    uint32_t n_pages, page_size, kv_heads, head_dim, format, dtype;
+} ckks_clear_packed_t;
+
+/* Writes the new tokens' keys and values into their pages; keys and queries are normed and rotated first:
+ *   with d_k_norm (d_q_norm), [head_dim] of norm_dtype (F32 or dtype):  x = x / sqrt(mean(x^2) + eps) * weight over each head's entries
+ *   rotation as in ckks_clear_cache_append
+ *   each block of 32 entries: e = the smallest number >= -100 with max |x| <= M 2^e, M = 448 (E4M3) or 127 (I8),
+ *   power = e + 127, codes = x / 2^e rounded to the nearest, ties to even.
+ * A block that holds an infinity, a NaN or an entry of 2^128 or more is stored as power 255 and codes 0.  Keys up to their code, and
+ * queries with a norm or a rotation, are computed in 64 bits: nothing is rounded on the way.  Rotated entries without an angle are
+ * NaN, and so is, in the cache, their block.  What is not stored, what may lie in what, rows in no sequence: as in
+ * ckks_clear_cache_append. */
+typedef struct {
+    ckks_clear_packed_t pages;
+    ckks_clear_batch_t batch;
+    const void *d_new_k, *d_new_v, *d_q;
+    void *d_q_out;
+    const void *d_k_norm, *d_q_norm;
+    const float *d_cos, *d_sin;
+    const int32_t *d_positions;
+    int64_t new_k_stride[2], new_v_stride[2], q_stride[2], q_out_stride[2];
+    uint32_t heads, rot, n_pos, flags, norm_dtype;
+    float eps; /* >= 0 */
+} ckks_clear_packed_append_t;
+int ckks_clear_packed_append(const ckks_clear_packed_append_t *a, void *stream);
+
+/* Attention of the new tokens over the packed pages, in every respect as ckks_clear_attend over pages that hold, in dtype, what the
+ * codes stand for (beyond its range F16 is infinite, as a conversion is). */
+typedef struct {
+    ckks_clear_packed_t pages;
+    ckks_clear_batch_t batch;
+    const void *d_q;
+    void *d_out;
+    float *d_lse;
+    void *d_work;
+    uint64_t work_bytes;
+    int64_t q_stride[2], out_stride[2];
+    uint32_t heads, window, flags;
+    float scale;
+} ckks_clear_packed_attend_t;
+uint64_t ckks_clear_packed_attend_work_bytes(const ckks_clear_packed_attend_t *a);
+int ckks_clear_packed_attend(const ckks_clear_packed_attend_t *a, void *stream);
+
+/* Reads the new tokens' keys and values (all of a sequence's, if as many rows as kv_len are asked for) back: the values that the codes
+ * stand for, in dtype.  A token at a position below 0 or in a page outside [0, n_pages) reads as zeros; rows in no sequence
+ * are not written.  Rows read and appended again give the same values.  d_k_out, d_v_out [n_tokens][kv_heads][head_dim] by strides
+ * {token, head}, either NULL; they share no entry. */
+typedef struct {
+    ckks_clear_packed_t pages;
+    ckks_clear_batch_t batch;
+    void *d_k_out, *d_v_out;
+    int64_t k_out_stride[2], v_out_stride[2];
+} ckks_clear_packed_read_t;
+int ckks_clear_packed_read(const ckks_clear_packed_read_t *a, void *stream);
+
+/* ---- the next token --------------------------------------------------------
+ * Draws a token of each row of logits l by a number u of [0, 1) that the caller gives:
+ *   w = exp((l - max l) / temperature)
+ *   top_k > 0:    the top_k tokens with the largest logits are kept (of equal ones the lowest ids)
+ *   top_p < 1:    of these, largest first, a token is kept while those before it sum to less than top_p times the sum of all of
+ *                 them (the first always is)
+ *   min_p > 0:    of these, a token is kept if w >= min_p  (1 or more: the largest ones)
+ *   token = the lowest id for which the sum of w over the kept tokens up to it exceeds u times the sum over all;
+ *   prob = its w over that sum
+ * d_temperature, d_top_p, d_min_p, d_u: f32 [rows], d_top_k: int32 [rows]; all but d_u may be NULL (1; no limit).  A
+ * temperature of 0 or below takes the largest logit (the lowest id; prob 1), top_p of 0 or below the first token only.  u below 0
+ * counts as 0, u of 1 or more takes the last token kept; NaN counts as no limit, temperature 1, u = 0.
+ * A logit of -infinity or NaN is never drawn; logits of +infinity are drawn alike.  A row without any other gets token -1, prob 0.
+ * Sums are held in 64 bits and joined in a fixed order: the same inputs give the same token.  d_prob: f32 [rows] or NULL. */
+typedef struct {
+    const void *d_logits;
+    int32_t *d_token;
+    float *d_prob;
+    const float *d_u, *d_temperature, *d_top_p, *d_min_p;
+    const int32_t *d_top_k;
+    int64_t logits_stride;
+    uint32_t rows, vocab, dtype, reserved;
+} ckks_clear_sample_t;
+int ckks_clear_sample(const ckks_clear_sample_t *a, void *stream);
 
 #ifdef __cplusplus
 }

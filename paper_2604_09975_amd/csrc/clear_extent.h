@@ -84,6 +84,17 @@ inline bool share(const Runs &a, const Runs &b) {
     return reaches((int64_t)((uintptr_t)a.at - (uintptr_t)b.at), a.run, s, n);
 }
 
+// share() for arrays whose runs differ in length: runs [p, p + m) and [q, q + n) meet where -m < p - q < n, which is where
+// 2 (p - q) - (n - m) lies between -(m + n) and m + n.
+inline bool share_any(const Runs &a, const Runs &b) {
+    Runs x = a, y = b;
+    const int64_t off = 2 * (int64_t)((uintptr_t)a.at - (uintptr_t)b.at) - (b.run - a.run);
+    x.at = (const void *)off, y.at = nullptr;
+    x.run = y.run = a.run + b.run;
+    for (int k = 0; k < 3; ++k) x.dim[k].stride *= 2, y.dim[k].stride *= 2;
+    return share(x, y);
+}
+
 // Two runs of one array share a byte.
 inline bool share_within(const Runs &a) {
     Step s[3];

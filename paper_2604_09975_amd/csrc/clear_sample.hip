@@ -2,21 +2,26 @@
 //
 // What is drawn depends on sums of up to a million weights compared with each other, so a weight is computed in 64 bits and added as a
 // whole number of 2^-bits: such sums do not depend on their order, and a token next to the border of two is off by 2^-40 of the sum at
-// most.  w = exp((l - max) / T) = 2^(n / 64) 2^f with n whole, |f| <= 1/128: a table of 64 and a polynomial of degree 4 (r^5 / 120
-// < 4e-14 for r = f ln 2).  Weights below 2^-64 are none.
+// most.  w = exp((l - max) / T) = 2^(-n / 256) 2^(f / 256) with n whole, |f| <= 1/2: a table of 256 and a polynomial of degree 3
+// (r^4 / 24 < 1.4e-13 for r = f ln 2 / 256).  Weights below 2^-64 are none.
 //
-// The order by logits is not needed, only where the kept tokens end in it.  One pass sums counts and weights into bins of
-// n / 2 (2^-1/32 apart).  The bin in which the top_k-th token, or the one that fills top_p, lies is then resolved: tokens of one
-// value by their count, few by their ranks, many by bins of their values again.  The draw sums the kept weights by stretches of ids and
-// looks into the one that holds u.
+// The order by logits is not needed, only where the kept tokens end in it: at a value, and after so many of the tokens that have it.
+//   top_k of up to 1024: the logits are counted by bins of their distance from the largest, those of the bins that hold the top_k are
+//     put into a list, and all the rest goes by the list.
+//   else: one pass sums counts and weights into bins (2^-1/32 apart).  The bin in which the top_k-th token, or the one that fills
+//     top_p, lies is then resolved: tokens of one value by their count, few by their ranks, many by bins of their values again.
+// The draw sums the kept weights by stretches of ids and looks into the one that holds u.
 #include <algorithm>
+#include <type_traits>
 
 #include "clear_device.h"
 
 namespace ckks {
 
-constexpr u32 THREADS = 1024, WAVES = THREADS / 64, BINS = 2048, LIST = 256, CHUNKS = 4096;
+constexpr u32 BINS = 2048, RANKED = 256, CHUNKS = 4096;
+constexpr u32 LIST_K = 1024, LISTED = 2048;  // the largest top_k that goes by a list, and the list's room
 constexpr u32 MAX_VOCAB = 1u << 20;
+constexpr u32 GRAIN = 256, GRAINS = 64 * GRAIN;  // steps of n: 2^-1/256; weights below 2^-64 are none
 
 struct SampleArgs {
     const void *logits;
@@ -28,288 +33,505 @@ struct SampleArgs {
     u32 vocab, bits;
 };
 
-__device__ __forceinline__ u32 low32(u64 x) { return (u32)x; }
-__device__ __forceinline__ u64 shfl_up64(u64 x, int by) {
-    return (u64)(u32)__shfl_up((u32)(x >> 32), by) << 32 | (u32)__shfl_up((u32)x, by);
+// Inclusive sums over the lanes of a wave: by DPP within rows of 16, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 add_dpp(u64 x) {
+    const u32 lo = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)x, CTRL, ROWS, 0xf, false);
+    const u32 hi = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(x >> 32), CTRL, ROWS, 0xf, false);
+    return x + ((u64)hi << 32 | lo);
 }
-// Inclusive sums over the lanes of a wave.
 __device__ __forceinline__ u64 scan_wave(u64 x) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 up = shfl_up64(x, o);
-        if ((threadIdx.x & 63) >= (u32)o) x += up;
-    }
-    return x;
+    x = add_dpp<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
+    x = add_dpp<0x112, 0xf>(x);
+    x = add_dpp<0x114, 0xf>(x);
+    x = add_dpp<0x118, 0xf>(x);
+    x = add_dpp<0x142, 0xa>(x);  // row_bcast 15, 31
+    return add_dpp<0x143, 0xc>(x);
 }
-// Inclusive sums over the block's threads; `wave_sums` is scratch of WAVES.
-__device__ __forceinline__ u64 scan_block(u64 x, u64 *wave_sums) {
-    x = scan_wave(x);
-    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    __syncthreads();
-    if (lane == 63) wave_sums[wave] = x;
-    __syncthreads();
-    u64 before = 0;
-    for (u32 w = 0; w < WAVES; ++w) before += w < wave ? wave_sums[w] : 0;
-    return x + before;
-}
-// The order of floats as that of whole numbers (-0 as 0).
+// The order of floats as that of whole numbers (-0 as 0), and back.
 __device__ __forceinline__ u32 key_of(float x) {
     const u32 b = __float_as_uint(x + 0.0f);
     return b >> 31 ? ~b : b | 1u << 31;
 }
+__device__ __forceinline__ float value_of(u32 key) { return __uint_as_float(key >> 31 ? key & ~(1u << 31) : ~key); }
 
-template <class T>
+// V: logits of an access, which a row has at least.
+template <class T, int THREADS, int V>
 __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
-    constexpr int V = 16 / sizeof(T);
-    constexpr u32 SPAN = THREADS * V;  // ids of a round
-    __shared__ u64 mass[CHUNKS];       // of the bins; of stretches of ids
-    __shared__ u32 count[BINS];
-    __shared__ double power[64];       // 2^(j / 64)
+    constexpr int PER = BINS / THREADS;
+    constexpr u32 SPAN = THREADS * V, WAVES = THREADS / 64;    // SPAN: ids of a round
+    __shared__ __attribute__((aligned(16))) u64 mass[CHUNKS];  // weights of the bins; of stretches of ids; lists
+    __shared__ u32 count[CHUNKS];                              // tokens of the bins; of stretches of ids that have the last value
+    __shared__ double power[GRAIN];                            // 2^(j / 256)
     __shared__ u64 wave_sums[WAVES];
-    __shared__ u32 list_key[LIST], list_id[LIST];
-    __shared__ u64 list_w[LIST];
+    __shared__ u32 list_key[RANKED], list_id[RANKED];
+    __shared__ u64 list_w[RANKED];
     __shared__ u32 n_list, key_min, key_max;
     __shared__ u32 found[4];
     __shared__ u64 found64[2];
     __shared__ float wave_top[WAVES];
-    u64 *const chunk = mass;
 
     const u32 row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const T *in = (const T *)a.logits + (i64)row * a.stride;
     const u32 rounds = (a.vocab + SPAN - 1) / SPAN;
-    auto fetch = [&](u32 r) {
-        const u32 c = r * SPAN + threadIdx.x * V;
-        Pack<T, V> x;
-        if (c + V <= a.vocab) return load_pack<V>(in + c);
+    // First id of the thread's part of a round; the last ones of a row begin before their place, and what lies there is left out.
+    auto at_of = [&](u32 r) { return min(r * SPAN + threadIdx.x * V, a.vocab - V); };
+    auto fetch = [&](u32 r) { return load_pack<V>(in + at_of(r)); };
+    auto cut = [&](u32 r, Pack<T, V> &x) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) x.v[i] = c + i < a.vocab ? in[c + i] : (T)-__builtin_inff();
-        return x;
+        for (int i = 0; i < V; ++i)
+            if (at_of(r) + i < r * SPAN + threadIdx.x * V) x.v[i] = (T)-__builtin_inff();
     };
-    // use(round, pack) for the thread's part of the row, the next round's under way
-    auto each = [&](auto use) {
-        Pack<T, V> next = fetch(0);
+    // use(first id, pack, round) for the thread's part of the row, `ahead` rounds under way.  (They keep their registers: moving a
+    // pack from one to another would be a wait for it.)
+    auto each = [&](auto ahead, auto use) {
+        constexpr u32 AHEAD = decltype(ahead)::value;
+        Pack<T, V> next[AHEAD];
+#pragma unroll
+        for (u32 k = 0; k < AHEAD; ++k) next[k] = fetch(k);
 #pragma unroll 1
-        for (u32 r = 0; r < rounds; ++r) {
-            const Pack<T, V> x = next;
-            next = fetch(r + 1);
-            use(r, x);
+        for (u32 r = 0; r < rounds; r += AHEAD)
+#pragma unroll
+            for (u32 k = 0; k < AHEAD; ++k) {
+                Pack<T, V> x = next[k];
+                next[k] = fetch(r + k + AHEAD);
+                if (r + k >= rounds) break;
+                if (r + k + 1 == rounds) cut(r + k, x);
+                use(at_of(r + k), x, r + k);
+            }
+    };
+    constexpr std::integral_constant<u32, 4> LIGHT;  // for passes that do little with a logit, and for the others
+    constexpr std::integral_constant<u32, 2> HEAVY;
+    // use(i, logit) for those few of a pack that `some` holds for: as many turns as the lane with the most of them has
+    auto few_of = [&](const Pack<T, V> &x, auto some, auto use) {
+        u32 bits = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) bits |= some((float)x.v[i]) ? 1u << i : 0u;
+        u32 w[4] = {0, 0, 0, 0};
+        __builtin_memcpy(w, &x, sizeof(x));
+        while (bits) {
+            const u32 i = __ffs(bits) - 1, at = i * sizeof(T) / 4;
+            bits &= bits - 1;
+            const u32 word = at & 2 ? (at & 1 ? w[3] : w[2]) : (at & 1 ? w[1] : w[0]), cell = word >> (i * sizeof(T) % 4 * 8);
+            T v;
+            __builtin_memcpy(&v, &cell, sizeof(T));
+            use(i, (float)v);
+        }
+    };
+    auto each_of = [&](auto some, auto use) {
+        each(LIGHT, [&](u32 at, const Pack<T, V> &x, u32) { few_of(x, some, [&](u32 i, float l) { use(at + i, l); }); });
+    };
+    // Inclusive sums over the threads.
+    auto scan_block = [&](u64 x) {
+        x = scan_wave(x);
+        __syncthreads();
+        if (lane == 63) wave_sums[wave] = x;
+        __syncthreads();
+        u64 before = 0;
+#pragma unroll
+        for (u32 w = 0; w < WAVES; ++w) before += w < wave ? wave_sums[w] : 0;
+        return x + before;
+    };
+    auto finish = [&](u32 token, double prob) {
+        if (threadIdx.x == 0) {
+            a.token[row] = (int32_t)token;
+            if (a.prob) a.prob[row] = (float)prob;
         }
     };
 
     float top = -__builtin_inff();
-    each([&](u32, const Pack<T, V> &x) {
+    each(LIGHT, [&](u32, const Pack<T, V> &x, u32) {
 #pragma unroll
         for (int i = 0; i < V; ++i) top = fmaxf(top, (float)x.v[i]);
     });
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (lane == 0) wave_top[wave] = top;
-    if (threadIdx.x < 64) power[threadIdx.x] = exp2(threadIdx.x / 64.0);
+    for (u32 j = threadIdx.x; j < GRAIN; j += THREADS) power[j] = exp2(j / (double)GRAIN);
+    for (u32 i = threadIdx.x; i < BINS; i += THREADS) mass[i] = 0, count[i] = 0;
+    if (threadIdx.x == 0) n_list = 0;
     __syncthreads();
 #pragma unroll
     for (u32 w = 0; w < WAVES; ++w) top = fmaxf(top, wave_top[w]);
-    if (top == -__builtin_inff()) {
-        if (threadIdx.x == 0) {
-            a.token[row] = -1;
-            if (a.prob) a.prob[row] = 0.0f;
-        }
-        return;
-    }
-    // logits as they count: NaN as -infinity; beside +infinity only such
-    const bool endless = top == __builtin_inff();
-    if (endless) top = 0.0f;
-    auto logit = [&](T x) {
-        const float l = fmaxf((float)x, -__builtin_inff());
-        return endless ? (l == __builtin_inff() ? 0.0f : -__builtin_inff()) : l;
-    };
+    if (top == -__builtin_inff()) return finish(~0u, 0.0);
 
-    float temperature = a.temperature ? a.temperature[row] : 1.0f;
-    const bool greedy = temperature <= 0.0f;
-    if (!(temperature > 0.0f)) temperature = 1.0f;
-    const double c64 = 64.0 * 1.4426950408889634074 / (double)temperature, top64 = top;
+    const float temperature = a.temperature && a.temperature[row] == a.temperature[row] ? a.temperature[row] : 1.0f;
+    const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f, u = a.u[row];
+    const int32_t top_k = a.top_k ? a.top_k[row] : 0;
+    const bool limit_k = top_k > 0 && (u32)top_k < a.vocab, limit_p = top_p < 1.0f;
+    const double least = min_p > 0.0f ? fmin((double)min_p, 1.0) : 0.0;
+    const double c = GRAIN * 1.4426950408889634074 / (double)temperature, top64 = top;
     const double magic = __longlong_as_double((long long)(1023 + 52 - a.bits) << 52);
-    constexpr double STEP = 0.69314718055994530942 / 64;
-    // 64 d and the weight of a logit, d = log2 of its inverse; none from 2^-64
+    // Logits that may have a weight; false for NaN and -infinity.  (A little below, so that it does not cut off what `weigh` counts.)
+    const float floor_l = fmaxf((float)(top64 - (GRAINS + 8.0) / c * (1 + 1e-6)), -3.402823466e38f);
+    auto may = [&](float l) { return l >= floor_l; };
+    const float reach = 1e-6f * fabsf(top);  // more than bounds that are worked out in 32 bits are off by
+    // n: steps down from the largest; w = 2^(-n / 256) 2^(f / 256).  NaN and all that is far below: n = GRAINS + 64.
     struct Weight {
         u32 n;
         double w;
-        __device__ bool some() const { return n < 2 * BINS; }
-    };
-    auto place = [&](float l, double &f) {
-        const double t = fmax(((double)l - top64) * c64, -8192.0), n = __builtin_rint(t);
-        f = t - n;
-        return (u32)-(int)n;
     };
     auto weigh = [&](float l) {
-        Weight r;
-        double f;
-        r.n = place(l, f);
-        f *= STEP;
-        const double e = __builtin_fma(f, __builtin_fma(f, __builtin_fma(f, __builtin_fma(f, 1.0 / 24, 1.0 / 6), 0.5), 1.0), 1.0);
-        const int n = -(int)r.n;
-        r.w = r.some() ? __builtin_ldexp(e * power[n & 63], n >> 6) : 0.0;
-        return r;
+        constexpr double ROUND = 6755399441055744.0, STEP = 0.69314718055994530942 / GRAIN;  // 1.5 * 2^52: n in the lower word of the sum
+        const double t = fmax(((double)l - top64) * c, -(double)(GRAINS + 64)), s = t + ROUND, f = t - (s - ROUND);
+        const double q = f * __builtin_fma(f, __builtin_fma(f, STEP * STEP * STEP / 6, STEP * STEP / 2), STEP);
+        const int n = (int)(u32)__double_as_longlong(s);
+        const u64 e = (u64)__double_as_longlong(power[n & (GRAIN - 1)]) + ((u64)(u32)((n >> 8) << 20) << 32);
+        const double p = __longlong_as_double((long long)e);
+        return Weight{(u32)-n, __builtin_fma(p, q, p)};
     };
+    static_assert(GRAIN == 256, "n >> 8");
+    auto bin_of = [&](u32 n) { return n / (GRAINS / BINS); };
+    // (0 from 2^-52 on, as `bits` is 51 at most)
     auto whole = [&](double w) { return (u64)__double_as_longlong(w + magic) & ((1ull << 52) - 1); };
+    // What u asks for of a sum.
+    auto share = [&](u64 sum) -> u64 { return u < 1.0f ? min((u64)(fmax((double)u, 0.0) * (double)sum), sum - 1) : u >= 1.0f ? sum - 1 : 0ull; };
 
-    // The lowest id with sum over ids up to it of amount(id, logit) above `target`; `all` becomes the sum over all ids.
-    auto by_id = [&](auto amount, auto target, u64 &all, u64 &own) -> u32 {
+    // Kept are the tokens above `last`, and of those that have it the `ties` with the lowest ids.
+    float last = floor_l;
+    u64 ties = ~0ull;
+
+    // The lowest id up to which amounts sum to more than goal(all of them): amount(logit) where `some` holds, and `one` for each of the
+    // first `ties` tokens of value `last` (for which `some` need not hold).  `dense`: most logits have an amount.  prob: the
+    // token's share.
+    auto draw = [&](auto dense, auto some, auto amount, u64 one, auto goal, double &prob) -> u32 {
+        constexpr bool DENSE = decltype(dense)::value;
+        auto value = [&](u64 sum, u64 n) { return sum + min(n, ties) * one; };
         __syncthreads();
-        each([&](u32 r, const Pack<T, V> &x) {
+        each(std::integral_constant<u32, DENSE ? 2 : 4>(), [&](u32, const Pack<T, V> &x, u32 r) {
             u64 sum = 0;
+            u32 same = 0;
+            if (DENSE) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum += amount(r * SPAN + threadIdx.x * V + i, logit(x.v[i]));
-            if (__any(sum != 0)) sum = scan_wave(sum);
-            if (lane == 63) chunk[r * WAVES + wave] = sum;
+                for (int i = 0; i < V; ++i) {
+                    sum += amount((float)x.v[i]);
+                    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                few_of(x, [&](float l) { return l >= last && some(l); }, [&](u32, float l) {
+                    if (l > last)
+                        sum += amount(l);
+                    else
+                        ++same;
+                });
+            }
+            if (DENSE || __any(sum != 0)) sum = scan_wave(sum);
+            if (!DENSE && __any(same != 0)) same = (u32)scan_wave(same);
+            if (lane == 63) {
+                mass[r * WAVES + wave] = sum;
+                count[r * WAVES + wave] = same;
+            }
         });
         __syncthreads();
-        // four chunks a thread
+        constexpr u32 EACH = THREADS == 1024 ? CHUNKS / THREADS : 1;  // chunks a thread
         const u32 n = rounds * WAVES;
-        u64 part[CHUNKS / THREADS], sum = 0;
+        u64 part[EACH], sum = 0;
+        u32 same[EACH], sames = 0;
 #pragma unroll
-        for (u32 k = 0; k < CHUNKS / THREADS; ++k) {
-            const u32 at = threadIdx.x * (CHUNKS / THREADS) + k;
-            part[k] = at < n ? chunk[at] : 0;
+        for (u32 k = 0; k < EACH; ++k) {
+            const u32 at = threadIdx.x * EACH + k;
+            part[k] = at < n ? mass[at] : 0;
+            same[k] = at < n ? count[at] : 0;
             sum += part[k];
+            sames += same[k];
         }
-        const u64 upto = scan_block(sum, wave_sums);
-        if (threadIdx.x == THREADS - 1) found64[0] = upto;
+        u64 sum0 = scan_block(sum);
+        u64 same0 = DENSE ? 0 : scan_block(sames);
+        if (threadIdx.x == THREADS - 1) found64[0] = value(sum0, same0);
+        sum0 -= sum;
+        same0 -= sames;
         __syncthreads();
-        all = found64[0];
-        const u64 goal = target(all);
-        u64 before = upto - sum;
+        const u64 all = found64[0], wanted = goal(all);
+        __syncthreads();
 #pragma unroll
-        for (u32 k = 0; k < CHUNKS / THREADS; ++k) {
-            if (before <= goal && goal < before + part[k]) {
-                found[0] = threadIdx.x * (CHUNKS / THREADS) + k;
-                found64[1] = before;
+        for (u32 k = 0; k < EACH; ++k) {
+            if (value(sum0, same0) <= wanted && wanted < value(sum0 + part[k], same0 + same[k])) {
+                found[0] = threadIdx.x * EACH + k;
+                found64[0] = sum0;
+                found64[1] = same0;
             }
-            before += part[k];
+            sum0 += part[k];
+            same0 += same[k];
         }
         __syncthreads();
         const u32 at = min(found[0], n - 1);
+        const u64 sum1 = found64[0], same1 = found64[1];
+        __syncthreads();
         if (wave == at % WAVES) {
             const u32 r = at / WAVES;
-            const Pack<T, V> x = fetch(r);
+            Pack<T, V> x = fetch(r);
+            cut(r, x);
             u64 part[V], sum = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) sum += part[i] = amount(r * SPAN + threadIdx.x * V + i, logit(x.v[i]));
-            u64 before = found64[1] + scan_wave(sum) - sum;
+            u32 same[V], sames = 0;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                if (before <= goal && goal < before + part[i]) {
-                    found[1] = r * SPAN + threadIdx.x * V + i;
-                    found64[0] = part[i];
+                const float l = (float)x.v[i];
+                const bool in = DENSE || (l >= last && some(l));
+                part[i] = in && (DENSE || l > last) ? amount(l) : 0;
+                same[i] = !DENSE && in && l == last;
+                sum += part[i];
+                sames += same[i];
+            }
+            u64 s = sum1 + scan_wave(sum) - sum, m = same1 + scan_wave(sames) - sames;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const u64 before = value(s, m), after = value(s + part[i], m + same[i]);
+                if (before <= wanted && wanted < after) {
+                    found[1] = at_of(r) + i;
+                    found64[0] = after - before;
                 }
-                before += part[i];
+                s += part[i];
+                m += same[i];
             }
         }
         __syncthreads();
-        own = found64[0];
+        prob = (double)found64[0] / (double)all;
         return found[1];
     };
+    constexpr std::false_type SPARSE;
+    constexpr std::true_type ALL;
 
-    // The last token kept in the order of logits: larger ones are, of equal ones those up to its id.
-    float last = -__builtin_inff();
-    u32 last_id = ~0u;
-    auto kept = [&](float l, u32 id) { return l > last || (l == last && id <= last_id); };
-    u64 all, own;
-    const int32_t top_k = a.top_k ? a.top_k[row] : 0;
-    const float top_p = a.top_p ? a.top_p[row] : 1.0f, min_p = a.min_p ? a.min_p[row] : 0.0f;
-    const bool limit_k = top_k > 0 && (u32)top_k < a.vocab, limit_p = top_p < 1.0f;
-    if (greedy || (limit_k && top_k == 1)) {
+    double prob;
+    const bool endless = top == __builtin_inff();  // beside +infinity nothing else counts
+    if (temperature <= 0.0f || (limit_k && top_k == 1) || endless) {
+        // the largest ones have the same weight: the first of them, or one of the first that the limits leave
         last = top;
-        last_id = by_id([&](u32, float l) { return l == top ? 1ull : 0ull; }, [](u64) { return 0ull; }, all, own);
-        if (threadIdx.x == 0) {
-            a.token[row] = (int32_t)last_id;
-            if (a.prob) a.prob[row] = 1.0f;
-        }
-        return;
+        const bool first = temperature <= 0.0f;
+        const u32 id = draw(
+            SPARSE, [&](float) { return true; }, [&](float) { return 0ull; }, 1,
+            [&](u64 n) {
+                if (limit_k) n = min(n, (u64)top_k);
+                if (limit_p) n = (u64)fmax(ceil((double)top_p * (double)n), 1.0);
+                ties = first ? 1 : n;
+                return share(ties);
+            },
+            prob);
+        return finish(id, ties == ~0ull ? 1.0 : 1.0 / (double)ties);
     }
-    if (limit_k || limit_p) {
-        // counts and weights by bins
-        for (u32 i = threadIdx.x; i < BINS; i += THREADS) mass[i] = 0, count[i] = 0;
-        __syncthreads();
-        each([&](u32, const Pack<T, V> &x) {
+
+    if (limit_k && (u32)top_k <= LIST_K) {
+        const float inv = (float)(c * (1.0 / (GRAINS / BINS)));
+        auto slot = [&](float l) { return (u32)fminf((top - l) * inv, (float)(BINS - 1)); };  // (NaN: the last)
+        each(LIGHT, [&](u32, const Pack<T, V> &x, u32) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const Weight w = weigh(logit(x.v[i]));
-                if (w.some()) {
-                    atomicAdd((unsigned long long *)&mass[w.n >> 1], (unsigned long long)whole(w.w));
-                    atomicAdd(&count[w.n >> 1], 1u);
-                }
+                const float l = (float)x.v[i];
+                if (may(l)) atomicAdd(&count[slot(l)], 1u);
             }
         });
         __syncthreads();
-        u64 bin_mass[2], upto_mass[2];
-        u32 bin_count[2], upto_count[2];
-        {
-            const u32 b = 2 * threadIdx.x;
+        u32 n[PER], sum = 0;
 #pragma unroll
-            for (int k = 0; k < 2; ++k) bin_mass[k] = mass[b + k], bin_count[k] = count[b + k];
-            upto_mass[1] = scan_block(bin_mass[0] + bin_mass[1], wave_sums);
-            upto_mass[0] = upto_mass[1] - bin_mass[1];
-            upto_count[1] = (u32)scan_block(bin_count[0] + bin_count[1], wave_sums);
-            upto_count[0] = upto_count[1] - bin_count[1];
+        for (int k = 0; k < PER; ++k) sum += n[k] = count[PER * threadIdx.x + k];
+        u32 upto = (u32)scan_block(sum) - sum;
+        if (threadIdx.x == THREADS - 1) found[0] = BINS - 1, found[1] = upto + sum;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (upto < (u32)top_k && (u32)top_k <= upto + n[k]) {
+                found[0] = PER * threadIdx.x + k;
+                found[1] = upto + n[k];
+            }
+            upto += n[k];
         }
+        __syncthreads();
+        const u32 bin = found[0], listed = found[1];
+        if (listed <= LISTED) {
+            u64 *const list = mass, *const weight = mass + LISTED;  // by order; weights by rank
+            const float lo = bin == BINS - 1 ? floor_l : top - (float)(bin + 1) / inv * 1.000001f - reach;
+            each_of([&](float l) { return may(l) && !(l < lo); },
+                    [&](u32 id, float l) {
+                        if (slot(l) <= bin) list[atomicAdd(&n_list, 1u)] = (u64)key_of(l) << 32 | (u32)~id;
+                    });
+            __syncthreads();
+            // Sorts `size` (a power of two) numbers, largest first.
+            auto sort = [&](u32 size) {
+                for (u32 k = 2; k <= size; k *= 2)
+                    for (u32 j = k / 2; j; j /= 2) {
+                        for (u32 i = threadIdx.x; i < size / 2; i += THREADS) {
+                            const u32 p = 2 * i - (i & (j - 1)), q = p + j;
+                            const u64 x = list[p], y = list[q];
+                            if ((x < y) == !(p & k)) list[p] = y, list[q] = x;
+                        }
+                        __syncthreads();
+                    }
+            };
+            u32 size = 64;
+            while (size < listed) size *= 2;
+            for (u32 i = listed + threadIdx.x; i < size; i += THREADS) list[i] = 0;
+            __syncthreads();
+            sort(size);
+            // consecutive ranks a thread
+            constexpr u32 EACH = LIST_K / THREADS;
+            const u32 kept = min((u32)top_k, listed);
+            u64 w[EACH], sum = 0;
+            u32 id[EACH];
+#pragma unroll
+            for (u32 k = 0; k < EACH; ++k) {
+                const u32 rank = threadIdx.x * EACH + k;
+                const u64 at = rank < kept ? list[rank] : 0;
+                id[k] = ~(u32)at;
+                const Weight x = weigh(value_of((u32)(at >> 32)));
+                w[k] = rank < kept && x.w >= least ? whole(x.w) : 0;
+                // top_p goes by all of them, whatever min_p leaves
+                sum += rank < kept ? whole(x.w) : 0;
+            }
+            u64 before = scan_block(sum);
+            if (threadIdx.x == THREADS - 1) found64[0] = before;
+            before -= sum;
+            __syncthreads();
+            const double limit = limit_p ? fmax((double)top_p * (double)found64[0], 0.5) : __builtin_inf();
+            sum = 0;
+#pragma unroll
+            for (u32 k = 0; k < EACH; ++k) {
+                const u32 rank = threadIdx.x * EACH + k;
+                const u64 own = rank < kept ? whole(weigh(value_of((u32)(list[rank] >> 32))).w) : 0;
+                if (!((double)before < limit)) w[k] = 0;
+                before += own;
+                sum += w[k];
+                if (rank < kept) weight[rank] = w[k];
+            }
+            __syncthreads();
+            // by ids
+            u32 many = 64;
+            while (many < kept) many *= 2;
+#pragma unroll
+            for (u32 k = 0; k < EACH; ++k) {
+                const u32 rank = threadIdx.x * EACH + k;
+                if (rank < many) list[rank] = rank < kept ? (u64)(u32)~id[k] << 32 | rank : 0;
+            }
+            __syncthreads();
+            sort(many);
+            sum = 0;
+#pragma unroll
+            for (u32 k = 0; k < EACH; ++k) {
+                const u32 rank = threadIdx.x * EACH + k;
+                const u64 at = rank < kept ? list[rank] : 0;
+                id[k] = ~(u32)(at >> 32);
+                w[k] = rank < kept ? weight[(u32)at] : 0;
+                sum += w[k];
+            }
+            before = scan_block(sum);
+            if (threadIdx.x == THREADS - 1) found64[0] = before;
+            before -= sum;
+            __syncthreads();
+            const u64 all = found64[0], wanted = share(all);
+#pragma unroll
+            for (u32 k = 0; k < EACH; ++k) {
+                if (before <= wanted && wanted < before + w[k]) {
+                    a.token[row] = (int32_t)id[k];
+                    if (a.prob) a.prob[row] = (float)((double)w[k] / (double)all);
+                }
+                before += w[k];
+            }
+            return;
+        }
+        // too many near the border of the top_k
+        for (u32 i = threadIdx.x; i < BINS; i += THREADS) count[i] = 0;
+        __syncthreads();
+    }
+
+    if (limit_k || limit_p) {
+        // counts and weights by bins
+        each(HEAVY, [&](u32, const Pack<T, V> &x, u32) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float l = (float)x.v[i];
+                if (may(l)) {
+                    const Weight w = weigh(l);
+                    if (w.n < GRAINS) {
+                        atomicAdd((unsigned long long *)&mass[bin_of(w.n)], (unsigned long long)whole(w.w));
+                        if (limit_k) atomicAdd(&count[bin_of(w.n)], 1u);
+                    }
+                }
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+        __syncthreads();
+        struct Bins {  // the thread's: what is in each, and in all up to each
+            u64 mass[PER], upto_mass[PER];
+            u32 count[PER], upto_count[PER];
+        };
+        auto scan_bins = [&](u64 m0, u32 c0) {  // m0, c0: what lies above them
+            Bins b;
+            u64 m = 0;
+            u32 n = 0;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                b.mass[k] = mass[PER * threadIdx.x + k], b.count[k] = count[PER * threadIdx.x + k];
+                m += b.mass[k], n += b.count[k];
+            }
+            m = m0 + scan_block(m) - m;
+            n = c0 + (u32)scan_block(n) - n;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) b.upto_mass[k] = m += b.mass[k], b.upto_count[k] = n += b.count[k];
+            return b;
+        };
+        const Bins bins = scan_bins(0, 0);
         if (threadIdx.x == THREADS - 1) {
-            found64[0] = upto_mass[1];
-            found[0] = upto_count[1];
+            found64[0] = bins.upto_mass[PER - 1];
+            found[0] = bins.upto_count[PER - 1];
         }
         __syncthreads();
         u64 total = found64[0];
         const u32 tokens = found[0];
         // Narrows to the last token that counts: with `by_count` the goal_count-th, else the one before which weights sum to less than
-        // goal_mass and with which they do not.  Sets last, last_id; returns the weights up to and with it.
+        // goal_mass and with which they do not.  Lowers the tokens kept to those up to it; returns the weights up to and with it.
         auto resolve = [&](bool by_count, u64 goal_count, double goal_mass) -> u64 {
-            const auto reached = [&](u64 c, u64 m) { return by_count ? c >= goal_count : (double)m >= goal_mass; };
-            __syncthreads();
-            if (threadIdx.x == 0) found[0] = ~0u;
-            __syncthreads();
+            const auto reached = [&](u64 n, u64 m) { return by_count ? n >= goal_count : (double)m >= goal_mass; };
+            const auto lower = [&](float l, u64 n) {
+                if (l > last)
+                    last = l, ties = n;
+                else if (l == last)
+                    ties = min(ties, n);
+            };
+            auto find = [&](const Bins &b) {
+                __syncthreads();
+                if (threadIdx.x == 0) found[0] = ~0u;
+                __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
-                if (reached(upto_count[k], upto_mass[k]) && !reached(upto_count[k] - bin_count[k], upto_mass[k] - bin_mass[k])) {
-                    found[0] = 2 * threadIdx.x + k;
-                    found[1] = upto_count[k] - bin_count[k];
-                    found64[0] = upto_mass[k] - bin_mass[k];
+                for (int k = 0; k < PER; ++k) {
+                    const u32 n = b.upto_count[k] - b.count[k];
+                    const u64 m = b.upto_mass[k] - b.mass[k];
+                    if (reached(b.upto_count[k], b.upto_mass[k]) && !reached(n, m)) {
+                        found[0] = PER * threadIdx.x + k;
+                        found[1] = n;
+                        found64[0] = m;
+                    }
                 }
-            __syncthreads();
+                __syncthreads();
+            };
+            find(bins);
             const u32 bin = found[0];
             u64 above_count = found[1], above_mass = found64[0];
-            if (bin == ~0u) {  // all of them count
-                last = -__builtin_inff();
-                last_id = ~0u;
-                return total;
-            }
-            u32 lo = 0, hi = ~0u;  // keys that are looked at
+            if (bin == ~0u) return total;  // all of them count
+            // logits of the bin, and a little beside it; if c is 0 they are NaN, and the comparisons below let all pass
+            const float lo = (float)(top64 - ((bin + 1) * (GRAINS / BINS) + 0.5) / c) - reach, hi = (float)(top64 - (bin * (GRAINS / BINS) - 1.0) / c) + reach;
+            auto near_bin = [&](float l) { return may(l) && !(l < lo) && !(l > hi); };
+            u32 from = 0, to = ~0u;  // keys that are looked at
             for (;;) {
                 __syncthreads();
                 if (threadIdx.x == 0) n_list = 0, key_min = ~0u, key_max = 0;
                 __syncthreads();
-                each([&](u32 r, const Pack<T, V> &x) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float l = logit(x.v[i]);
-                        double f;
-                        const u32 key = key_of(l);
-                        if (place(l, f) >> 1 == bin && key >= lo && key <= hi) {
-                            atomicMin(&key_min, key);
-                            atomicMax(&key_max, key);
-                            const u32 at = atomicAdd(&n_list, 1u);
-                            if (at < LIST) {
-                                list_key[at] = key;
-                                list_id[at] = r * SPAN + threadIdx.x * V + i;
-                                list_w[at] = whole(weigh(l).w);
-                            }
-                        }
+                each_of(near_bin, [&](u32 id, float l) {
+                    const u32 key = key_of(l);
+                    const Weight w = weigh(l);
+                    if (bin_of(w.n) != bin || key < from || key > to) return;
+                    atomicMin(&key_min, key);
+                    atomicMax(&key_max, key);
+                    const u32 at = atomicAdd(&n_list, 1u);
+                    if (at < RANKED) {
+                        list_key[at] = key;
+                        list_id[at] = id;
+                        list_w[at] = whole(w.w);
                     }
                 });
                 __syncthreads();
-                const u32 n = n_list, from = key_min, to = key_max;
-                const auto value = [](u32 key) { return __uint_as_float(key >> 31 ? key & ~(1u << 31) : ~key); };
-                if (from == to) {  // equal ones: by their ids
-                    last = value(from);
-                    const u64 w = whole(weigh(last).w);
+                const u32 n = n_list;
+                from = key_min, to = key_max;
+                if (from == to) {  // equal ones: so many of them
+                    const float l = value_of(from);
+                    const u64 w = whole(weigh(l).w);
                     u64 m;
                     if (by_count) {
                         m = goal_count - above_count;
@@ -319,30 +541,31 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                         while (m < n && (double)(above_mass + m * w) < goal_mass) ++m;
                     }
                     m = min(max(m, 1ull), (u64)n);
-                    u64 sum, one;
-                    const float at = last;
-                    last_id = by_id([&](u32, float l) { return l == at ? 1ull : 0ull; }, [&](u64) { return m - 1; }, sum, one);
+                    lower(l, m);
                     return above_mass + m * w;
                 }
-                if (n <= LIST) {  // by their ranks
+                if (n <= RANKED) {  // by their ranks
                     if (threadIdx.x < n) {
                         const u32 key = list_key[threadIdx.x], id = list_id[threadIdx.x];
                         const u64 w = list_w[threadIdx.x];
-                        u64 c = above_count, m = above_mass;
-                        for (u32 j = 0; j < n; ++j)
-                            if (list_key[j] > key || (list_key[j] == key && list_id[j] < id)) {
-                                ++c;
+                        u64 before = above_count, m = above_mass;
+                        u32 same = 1;
+                        for (u32 j = 0; j < n; ++j) {
+                            const bool tie = list_key[j] == key && list_id[j] < id;
+                            if (list_key[j] > key || tie) {
+                                ++before;
                                 m += list_w[j];
                             }
-                        if (!reached(c, m) && reached(c + 1, m + w)) {
+                            same += tie;
+                        }
+                        if (!reached(before, m) && reached(before + 1, m + w)) {
                             found[2] = key;
-                            found[3] = id;
+                            found[3] = same;
                             found64[1] = m + w;
                         }
                     }
                     __syncthreads();
-                    last = value(found[2]);
-                    last_id = found[3];
+                    lower(value_of(found[2]), found[3]);
                     return found64[1];
                 }
                 // by bins of their keys
@@ -350,66 +573,52 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                 while ((to - from) >> shift >= BINS) ++shift;
                 for (u32 i = threadIdx.x; i < BINS; i += THREADS) mass[i] = 0, count[i] = 0;
                 __syncthreads();
-                each([&](u32, const Pack<T, V> &x) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float l = logit(x.v[i]);
-                        double f;
-                        const u32 key = key_of(l);
-                        if (place(l, f) >> 1 == bin && key >= from && key <= to) {
-                            atomicAdd((unsigned long long *)&mass[(to - key) >> shift], (unsigned long long)whole(weigh(l).w));
-                            atomicAdd(&count[(to - key) >> shift], 1u);
-                        }
-                    }
+                each_of(near_bin, [&](u32, float l) {
+                    const u32 key = key_of(l);
+                    const Weight w = weigh(l);
+                    if (bin_of(w.n) != bin || key < from || key > to) return;
+                    atomicAdd((unsigned long long *)&mass[(to - key) >> shift], (unsigned long long)whole(w.w));
+                    atomicAdd(&count[(to - key) >> shift], 1u);
                 });
                 __syncthreads();
-                const u64 m0 = mass[2 * threadIdx.x], m1 = mass[2 * threadIdx.x + 1];
-                const u32 c0 = count[2 * threadIdx.x], c1 = count[2 * threadIdx.x + 1];
-                const u64 um = above_mass + scan_block(m0 + m1, wave_sums), uc = above_count + scan_block(c0 + c1, wave_sums);
-                auto take = [&](u32 b, u64 c, u64 m, u64 dc, u64 dm) {
-                    if (reached(c, m) && !reached(c - dc, m - dm)) {
-                        found[0] = b;
-                        found[1] = (u32)(c - dc);
-                        found64[0] = m - dm;
-                    }
-                };
-                take(2 * threadIdx.x, uc - c1, um - m1, c0, m0);
-                take(2 * threadIdx.x + 1, uc, um, c1, m1);
-                __syncthreads();
+                find(scan_bins(above_mass, (u32)above_count));
                 above_count = found[1];
                 above_mass = found64[0];
-                hi = to - (found[0] << shift);
+                to -= min(found[0], BINS - 1) << shift;
                 const u32 width = (1u << shift) - 1;
-                lo = hi - from > width ? hi - width : from;
+                from = to - from > width ? to - width : from;
             }
         };
         if (limit_k && (u32)top_k < tokens) total = resolve(true, (u64)top_k, 0.0);
-        if (limit_p) {
-            const float l = last;
-            const u32 id = last_id;
-            resolve(false, 0, fmax((double)top_p * (double)total, 0.5));
-            // (within the top_k already, but for a goal that rounds to all of them)
-            if (l > last || (l == last && id < last_id)) last = l, last_id = id;
-        }
+        if (limit_p) resolve(false, 0, fmax((double)top_p * (double)total, 0.5));
     }
-    const double least = min_p > 0.0f ? fmin((double)min_p, 1.0) : 0.0;
-    const float u = a.u[row];
-    const u32 id = by_id(
-        [&](u32 i, float l) -> u64 {
-            if (!kept(l, i)) return 0;
-            const Weight w = weigh(l);
-            return w.w >= least ? whole(w.w) : 0ull;
-        },
-        [&](u64 sum) -> u64 { return u < 1.0f ? min((u64)(fmax((double)u, 0.0) * (double)sum), sum - 1) : u >= 1.0f ? sum - 1 : 0ull; }, all, own);
-    if (threadIdx.x == 0) {
-        a.token[row] = (int32_t)id;
-        if (a.prob) a.prob[row] = (float)((double)own / (double)all);
+    u32 id;
+    if (last > floor_l || ties != ~0ull || least > 0.0) {
+        // logits that may reach min_p, and a little below
+        const float enough = least > 0.0 ? (float)(top64 + (__log2f((float)least) * GRAIN - 1.0) / c) - reach : last;
+        const double w = weigh(last).w;
+        id = draw(
+            SPARSE, [&](float l) { return !(l < enough); },
+            [&](float l) -> u64 {
+                const double w = weigh(l).w;
+                return w >= least ? whole(w) : 0ull;
+            },
+            w >= least ? whole(w) : 0ull, share, prob);
+    } else {
+        id = draw(ALL, may, [&](float l) { return whole(weigh(l).w); }, 0, share, prob);
     }
+    finish(id, prob);
 }
 
 template <class T>
 static void launch_sample(const SampleArgs &a, u32 rows, hipStream_t st) {
-    hipLaunchKernelGGL((sample_kernel<T>), dim3(rows), dim3(THREADS), 0, st, a);
+    constexpr u32 V = 16 / sizeof(T);
+    if (a.vocab < V)
+        hipLaunchKernelGGL((sample_kernel<T, 256, 1>), dim3(rows), dim3(256), 0, st, a);
+    else if (a.vocab <= 256 * V * 4)
+        hipLaunchKernelGGL((sample_kernel<T, 256, V>), dim3(rows), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((sample_kernel<T, 1024, V>), dim3(rows), dim3(1024), 0, st, a);
 }
 
 }  // namespace ckks

@@ -9,7 +9,7 @@
 //   top_k of up to 1024: the logits are counted by bins of their distance from the largest, those of the bins that hold the top_k are
 //     put into a list, and all the rest goes by the list.
 //   else: one pass sums counts and weights into bins (2^-1/32 apart).  The bin in which the top_k-th token, or the one that fills
-//     top_p, lies is then resolved: tokens of one value by their count, few by their ranks, many by bins of their values again.
+//     top_p, lies is then resolved: tokens of one value by their count, others by sorting them, very many by bins of their values first.
 // The draw sums the kept weights by stretches of ids and looks into the one that holds u.
 #include <algorithm>
 #include <type_traits>
@@ -18,7 +18,7 @@
 
 namespace ckks {
 
-constexpr u32 BINS = 2048, RANKED = 256, CHUNKS = 4096;
+constexpr u32 BINS = 2048, CHUNKS = 4096;
 constexpr u32 LIST_K = 1024, LISTED = 2048;  // the largest top_k that goes by a list, and the list's room
 constexpr u32 MAX_VOCAB = 1u << 20;
 constexpr u32 GRAIN = 256, GRAINS = 64 * GRAIN;  // steps of n: 2^-1/256; weights below 2^-64 are none
@@ -59,14 +59,14 @@ __device__ __forceinline__ float value_of(u32 key) { return __uint_as_float(key 
 template <class T, int THREADS, int V>
 __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     constexpr int PER = BINS / THREADS;
+    constexpr u32 APART = THREADS == 1024 ? 8192 : 2048;
     constexpr u32 SPAN = THREADS * V, WAVES = THREADS / 64;    // SPAN: ids of a round
     __shared__ __attribute__((aligned(16))) u64 mass[CHUNKS];  // weights of the bins; of stretches of ids; lists
     __shared__ u32 count[CHUNKS];                              // tokens of the bins; of stretches of ids that have the last value
+    __shared__ u64 apart[APART];                               // tokens set apart, those that all later passes are about
     __shared__ double power[GRAIN];                            // 2^(j / 256)
     __shared__ u64 wave_sums[WAVES];
-    __shared__ u32 list_key[RANKED], list_id[RANKED];
-    __shared__ u64 list_w[RANKED];
-    __shared__ u32 n_list, key_min, key_max;
+    __shared__ u32 n_list, n_apart, n_bin, key_min, key_max;
     __shared__ u32 found[4];
     __shared__ u64 found64[2];
     __shared__ float wave_top[WAVES];
@@ -107,18 +107,29 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         u32 bits = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) bits |= some((float)x.v[i]) ? 1u << i : 0u;
-        u32 w[4] = {0, 0, 0, 0};
+        u32 w[8] = {};
         __builtin_memcpy(w, &x, sizeof(x));
         while (bits) {
             const u32 i = __ffs(bits) - 1, at = i * sizeof(T) / 4;
             bits &= bits - 1;
-            const u32 word = at & 2 ? (at & 1 ? w[3] : w[2]) : (at & 1 ? w[1] : w[0]), cell = word >> (i * sizeof(T) % 4 * 8);
+            const u32 a0 = at & 1 ? w[1] : w[0], a1 = at & 1 ? w[3] : w[2], a2 = at & 1 ? w[5] : w[4], a3 = at & 1 ? w[7] : w[6];
+            const u32 word = at & 4 ? (at & 2 ? a3 : a2) : (at & 2 ? a1 : a0), cell = word >> (i * sizeof(T) % 4 * 8);
             T v;
             __builtin_memcpy(&v, &cell, sizeof(T));
             use(i, (float)v);
         }
     };
+    bool set_apart = false;
     auto each_of = [&](auto some, auto use) {
+        if (set_apart) {
+            const u32 n = n_apart;
+            for (u32 i = threadIdx.x; i < n; i += THREADS) {
+                const u64 x = apart[i];
+                const float l = value_of((u32)(x >> 32));
+                if (some(l)) use((u32)~x, l);
+            }
+            return;
+        }
         each(LIGHT, [&](u32 at, const Pack<T, V> &x, u32) { few_of(x, some, [&](u32 i, float l) { use(at + i, l); }); });
     };
     // Inclusive sums over the threads.
@@ -144,12 +155,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) top = fmaxf(top, (float)x.v[i]);
     });
+    const float own_top = top;
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (lane == 0) wave_top[wave] = top;
     for (u32 j = threadIdx.x; j < GRAIN; j += THREADS) power[j] = exp2(j / (double)GRAIN);
     for (u32 i = threadIdx.x; i < BINS; i += THREADS) mass[i] = 0, count[i] = 0;
-    if (threadIdx.x == 0) n_list = 0;
+    if (threadIdx.x == 0) n_list = n_apart = 0;
     __syncthreads();
 #pragma unroll
     for (u32 w = 0; w < WAVES; ++w) top = fmaxf(top, wave_top[w]);
@@ -197,8 +209,18 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     auto draw = [&](auto dense, auto some, auto amount, u64 one, auto goal, double &prob) -> u32 {
         constexpr bool DENSE = decltype(dense)::value;
         auto value = [&](u64 sum, u64 n) { return sum + min(n, ties) * one; };
+        const u32 n = rounds * WAVES;  // a chunk: what a wave takes in a round, 64 V ids
         __syncthreads();
-        each(std::integral_constant<u32, DENSE ? 2 : 4>(), [&](u32, const Pack<T, V> &x, u32 r) {
+        if (!DENSE && set_apart) {
+            for (u32 i = threadIdx.x; i < n; i += THREADS) mass[i] = 0, count[i] = 0;
+            __syncthreads();
+            each_of([&](float l) { return l >= last && some(l); }, [&](u32 id, float l) {
+                if (l > last)
+                    atomicAdd((unsigned long long *)&mass[id / (64 * V)], (unsigned long long)amount(l));
+                else
+                    atomicAdd(&count[id / (64 * V)], 1u);
+            });
+        } else each(std::integral_constant<u32, DENSE ? 2 : 4>(), [&](u32, const Pack<T, V> &x, u32 r) {
             u64 sum = 0;
             u32 same = 0;
             if (DENSE) {
@@ -224,7 +246,6 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         });
         __syncthreads();
         constexpr u32 EACH = THREADS == 1024 ? CHUNKS / THREADS : 1;  // chunks a thread
-        const u32 n = rounds * WAVES;
         u64 part[EACH], sum = 0;
         u32 same[EACH], sames = 0;
 #pragma unroll
@@ -291,6 +312,48 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     constexpr std::false_type SPARSE;
     constexpr std::true_type ALL;
 
+    u64 *const list = mass, *const weight = mass + LISTED;  // tokens by their order: key, then the lower id; weights by rank
+    auto entry = [](u32 id, float l) { return (u64)key_of(l) << 32 | (u32)~id; };
+    // Few lanes at a time have a token for the list: each adds 1 for itself.  (An address that the compiler knows to be one for all
+    // lanes makes it sum over the wave first, which takes ten times as long.)
+    u32 zero = 0;
+    asm volatile("" : "+v"(zero));
+    auto enlist = [&](u32 id, float l) {
+        const u32 at = atomicAdd(&n_list + zero, 1u);
+        if (at < LISTED) list[at] = entry(id, l);
+    };
+    // Sorts `size` (a power of two) numbers, largest first.
+    auto sort = [&](u32 size) {
+        if (size <= 256) {  // by counting the larger ones, several threads to a number; they all differ but for the zeros behind them
+            const u32 parts = THREADS / size, at = threadIdx.x / parts, part = threadIdx.x % parts;
+            const u64 x = list[at];
+            u32 rank = 0;
+            for (u32 i = part; i < size; i += parts) rank += list[i] > x || (list[i] == x && i < at);
+            for (u32 o = 1; o < parts; o *= 2) rank += __shfl_xor(rank, o);
+            __syncthreads();
+            if (!part) list[rank] = x;
+            __syncthreads();
+            return;
+        }
+        for (u32 k = 2; k <= size; k *= 2)
+            for (u32 j = k / 2; j; j /= 2) {
+                for (u32 i = threadIdx.x; i < size / 2; i += THREADS) {
+                    const u32 p = 2 * i - (i & (j - 1)), q = p + j;
+                    const u64 x = list[p], y = list[q];
+                    if ((x < y) == !(p & k)) list[p] = y, list[q] = x;
+                }
+                __syncthreads();
+            }
+    };
+    // Fills the list up with what comes last and sorts it.
+    auto sort_list = [&](u32 n) {
+        u32 size = 64;
+        while (size < n) size *= 2;
+        for (u32 i = n + threadIdx.x; i < size; i += THREADS) list[i] = 0;
+        __syncthreads();
+        sort(size);
+    };
+
     double prob;
     const bool endless = top == __builtin_inff();  // beside +infinity nothing else counts
     if (temperature <= 0.0f || (limit_k && top_k == 1) || endless) {
@@ -312,55 +375,48 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     if (limit_k && (u32)top_k <= LIST_K) {
         const float inv = (float)(c * (1.0 / (GRAINS / BINS)));
         auto slot = [&](float l) { return (u32)fminf((top - l) * inv, (float)(BINS - 1)); };  // (NaN: the last)
-        each(LIGHT, [&](u32, const Pack<T, V> &x, u32) {
+        u32 listed = 0;
+        // As many threads as top_k have a logit at or above the top_k-th of the threads' largest, so the top_k are among those: mostly
+        // not many more.  If there are, all logits are counted.
+        for (u32 attempt = 0; attempt < 2; ++attempt) {
+            if (attempt) {
+                for (u32 i = threadIdx.x; i < BINS; i += THREADS) count[i] = 0;
+                __syncthreads();
+                each(LIGHT, [&](u32, const Pack<T, V> &x, u32) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float l = (float)x.v[i];
-                if (may(l)) atomicAdd(&count[slot(l)], 1u);
+                    for (int i = 0; i < V; ++i) {
+                        const float l = (float)x.v[i];
+                        if (may(l)) atomicAdd(&count[slot(l)], 1u);
+                    }
+                });
+            } else if (may(own_top)) {
+                atomicAdd(&count[slot(own_top)], 1u);
             }
-        });
-        __syncthreads();
-        u32 n[PER], sum = 0;
+            __syncthreads();
+            u32 n[PER], sum = 0;
 #pragma unroll
-        for (int k = 0; k < PER; ++k) sum += n[k] = count[PER * threadIdx.x + k];
-        u32 upto = (u32)scan_block(sum) - sum;
-        if (threadIdx.x == THREADS - 1) found[0] = BINS - 1, found[1] = upto + sum;
-        __syncthreads();
+            for (int k = 0; k < PER; ++k) sum += n[k] = count[PER * threadIdx.x + k];
+            u32 upto = (u32)scan_block(sum) - sum;
+            if (threadIdx.x == 0) found[0] = BINS - 1, n_list = 0;
+            __syncthreads();
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            if (upto < (u32)top_k && (u32)top_k <= upto + n[k]) {
-                found[0] = PER * threadIdx.x + k;
-                found[1] = upto + n[k];
+            for (int k = 0; k < PER; ++k) {
+                if (upto < (u32)top_k && (u32)top_k <= upto + n[k]) found[0] = PER * threadIdx.x + k;
+                upto += n[k];
             }
-            upto += n[k];
-        }
-        __syncthreads();
-        const u32 bin = found[0], listed = found[1];
-        if (listed <= LISTED) {
-            u64 *const list = mass, *const weight = mass + LISTED;  // by order; weights by rank
-            const float lo = bin == BINS - 1 ? floor_l : top - (float)(bin + 1) / inv * 1.000001f - reach;
-            each_of([&](float l) { return may(l) && !(l < lo); },
+            __syncthreads();
+            const u32 bin = found[0];
+            const float lo = bin == BINS - 1 ? floor_l : fmaxf(top - (float)(bin + 1) / inv * 1.000001f - reach, floor_l);
+            each_of([&](float l) { return l >= lo; },
                     [&](u32 id, float l) {
-                        if (slot(l) <= bin) list[atomicAdd(&n_list, 1u)] = (u64)key_of(l) << 32 | (u32)~id;
+                        if (slot(l) <= bin) enlist(id, l);
                     });
             __syncthreads();
-            // Sorts `size` (a power of two) numbers, largest first.
-            auto sort = [&](u32 size) {
-                for (u32 k = 2; k <= size; k *= 2)
-                    for (u32 j = k / 2; j; j /= 2) {
-                        for (u32 i = threadIdx.x; i < size / 2; i += THREADS) {
-                            const u32 p = 2 * i - (i & (j - 1)), q = p + j;
-                            const u64 x = list[p], y = list[q];
-                            if ((x < y) == !(p & k)) list[p] = y, list[q] = x;
-                        }
-                        __syncthreads();
-                    }
-            };
-            u32 size = 64;
-            while (size < listed) size *= 2;
-            for (u32 i = listed + threadIdx.x; i < size; i += THREADS) list[i] = 0;
-            __syncthreads();
-            sort(size);
+            listed = n_list;
+            if (listed <= LISTED) break;
+        }
+        if (listed <= LISTED) {
+            sort_list(listed);
             // consecutive ranks a thread
             constexpr u32 EACH = LIST_K / THREADS;
             const u32 kept = min((u32)top_k, listed);
@@ -427,7 +483,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             return;
         }
         // too many near the border of the top_k
-        for (u32 i = threadIdx.x; i < BINS; i += THREADS) count[i] = 0;
+        for (u32 i = threadIdx.x; i < BINS; i += THREADS) mass[i] = 0, count[i] = 0;
         __syncthreads();
     }
 
@@ -505,29 +561,55 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             const u32 bin = found[0];
             u64 above_count = found[1], above_mass = found64[0];
             if (bin == ~0u) return total;  // all of them count
-            // logits of the bin, and a little beside it; if c is 0 they are NaN, and the comparisons below let all pass
-            const float lo = (float)(top64 - ((bin + 1) * (GRAINS / BINS) + 0.5) / c) - reach, hi = (float)(top64 - (bin * (GRAINS / BINS) - 1.0) / c) + reach;
-            auto near_bin = [&](float l) { return may(l) && !(l < lo) && !(l > hi); };
+            // logits of the bin, and a little beside it
+            float lo = fmaxf((float)(top64 - ((bin + 1) * (GRAINS / BINS) + 0.5) / c) - reach, floor_l), hi = (float)(top64 - (bin * (GRAINS / BINS) - 1.0) / c) + reach;
+            if (!(c > 0.0)) lo = floor_l, hi = top;
+            if (!set_apart) {  // what is kept lies in this bin and above it
+                each_of([&](float l) { return l >= lo; }, [&](u32 id, float l) {
+                    const u32 at = atomicAdd(&n_apart + zero, 1u);
+                    if (at < APART) apart[at] = entry(id, l);
+                });
+                __syncthreads();
+                set_apart = n_apart <= APART;
+                __syncthreads();
+                if (!set_apart && threadIdx.x == 0) n_apart = 0;
+            }
+            auto near_bin = [&](float l) { return __builtin_amdgcn_fmed3f(l, lo, hi) == l; };
             u32 from = 0, to = ~0u;  // keys that are looked at
             for (;;) {
                 __syncthreads();
-                if (threadIdx.x == 0) n_list = 0, key_min = ~0u, key_max = 0;
+                if (threadIdx.x == 0) n_list = n_bin = 0, key_min = ~0u, key_max = 0;
                 __syncthreads();
+                const bool again = from || ~to;
                 each_of(near_bin, [&](u32 id, float l) {
                     const u32 key = key_of(l);
-                    const Weight w = weigh(l);
-                    if (bin_of(w.n) != bin || key < from || key > to) return;
-                    atomicMin(&key_min, key);
-                    atomicMax(&key_max, key);
-                    const u32 at = atomicAdd(&n_list, 1u);
-                    if (at < RANKED) {
-                        list_key[at] = key;
-                        list_id[at] = id;
-                        list_w[at] = whole(w.w);
-                    }
+                    if (!again || (key >= from && key <= to)) enlist(id, l);
                 });
                 __syncthreads();
-                const u32 n = n_list;
+                // those that are indeed of the bin, their number and the range of their keys
+                u32 n = n_list, low = ~0u, high = 0, mine = 0;
+                const bool fits = n <= LISTED;
+                auto look = [&](u32 key) {
+                    if (bin_of(weigh(value_of(key)).n) != bin) return false;
+                    low = min(low, key), high = max(high, key), ++mine;
+                    return true;
+                };
+                if (fits) {
+                    for (u32 i = threadIdx.x; i < n; i += THREADS)
+                        if (!look((u32)(list[i] >> 32))) list[i] = 0;
+                } else {
+                    each_of(near_bin, [&](u32, float l) {
+                        const u32 key = key_of(l);
+                        if (key >= from && key <= to) look(key);
+                    });
+                }
+                if (mine) {
+                    atomicMin(&key_min, low);
+                    atomicMax(&key_max, high);
+                    atomicAdd(&n_bin, mine);
+                }
+                __syncthreads();
+                const u32 members = n_bin;
                 from = key_min, to = key_max;
                 if (from == to) {  // equal ones: so many of them
                     const float l = value_of(from);
@@ -538,34 +620,44 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                     } else {  // the smallest m with above + m w >= goal
                         m = w ? (u64)((goal_mass - (double)above_mass) / (double)w) : 1;
                         while (m > 1 && (double)(above_mass + (m - 1) * w) >= goal_mass) --m;
-                        while (m < n && (double)(above_mass + m * w) < goal_mass) ++m;
+                        while (m < members && (double)(above_mass + m * w) < goal_mass) ++m;
                     }
-                    m = min(max(m, 1ull), (u64)n);
+                    m = min(max(m, 1ull), (u64)members);
                     lower(l, m);
                     return above_mass + m * w;
                 }
-                if (n <= RANKED) {  // by their ranks
-                    if (threadIdx.x < n) {
-                        const u32 key = list_key[threadIdx.x], id = list_id[threadIdx.x];
-                        const u64 w = list_w[threadIdx.x];
-                        u64 before = above_count, m = above_mass;
-                        u32 same = 1;
-                        for (u32 j = 0; j < n; ++j) {
-                            const bool tie = list_key[j] == key && list_id[j] < id;
-                            if (list_key[j] > key || tie) {
-                                ++before;
-                                m += list_w[j];
-                            }
-                            same += tie;
+                if (fits) {  // in their order
+                    sort_list(n);
+                    constexpr u32 EACH = LISTED / THREADS;
+                    u64 w[EACH], m = 0;
+#pragma unroll
+                    for (u32 k = 0; k < EACH; ++k) {
+                        const u32 rank = threadIdx.x * EACH + k;
+                        m += w[k] = rank < members ? whole(weigh(value_of((u32)(list[rank] >> 32))).w) : 0;
+                    }
+                    u64 before = above_mass + scan_block(m) - m;
+#pragma unroll
+                    for (u32 k = 0; k < EACH; ++k) {
+                        const u32 rank = threadIdx.x * EACH + k;
+                        const u64 at = above_count + rank;
+                        if (rank < members && !reached(at, before) && reached(at + 1, before + w[k])) {
+                            found[2] = rank;
+                            found64[1] = before + w[k];
                         }
-                        if (!reached(before, m) && reached(before + 1, m + w)) {
-                            found[2] = key;
-                            found[3] = same;
-                            found64[1] = m + w;
-                        }
+                        before += w[k];
                     }
                     __syncthreads();
-                    lower(value_of(found[2]), found[3]);
+                    // its place among its equals: the first of them by halves
+                    const u32 rank = min(found[2], members - 1), key = (u32)(list[rank] >> 32);
+                    u32 first = 0, end = rank;
+                    while (first < end) {
+                        const u32 mid = (first + end) / 2;
+                        if ((u32)(list[mid] >> 32) > key)
+                            first = mid + 1;
+                        else
+                            end = mid;
+                    }
+                    lower(value_of(key), rank - first + 1);
                     return found64[1];
                 }
                 // by bins of their keys
@@ -612,7 +704,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
 
 template <class T>
 static void launch_sample(const SampleArgs &a, u32 rows, hipStream_t st) {
-    constexpr u32 V = 16 / sizeof(T);
+    constexpr u32 V = 8;
     if (a.vocab < V)
         hipLaunchKernelGGL((sample_kernel<T, 256, 1>), dim3(rows), dim3(256), 0, st, a);
     else if (a.vocab <= 256 * V * 4)

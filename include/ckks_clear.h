@@ -180,8 +180,8 @@ typedef struct {
  *   rotation as in ckks_clear_cache_append
  *   each block of 32 entries: e = the smallest number >= -100 with max |x| <= M 2^e, M = 448 (E4M3) or 127 (I8),
  *   power = e + 127, codes = x / 2^e rounded to the nearest, ties to even.
- * A block that holds an infinity, a NaN or an entry of 2^128 or more is stored as power 255 and codes 0.  Keys up to their code, and
- * queries with a norm or a rotation, are computed in 64 bits: nothing is rounded on the way.  Rotated entries without an angle are
+ * A block that holds an infinity, a NaN or an entry of 2^128 or more is stored as power 255 and codes 0.  Norm and rotation are
+ * computed in 64 bits; keys meet no other rounding than that to their code, queries are rounded to 32 bits and to dtype.  Rotated entries without an angle are
  * NaN, and so is, in the cache, their block.  What is not stored, what may lie in what, rows in no sequence: as in
  * ckks_clear_cache_append. */
 typedef struct {

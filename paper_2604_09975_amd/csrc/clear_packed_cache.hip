@@ -1,7 +1,7 @@
 // New keys and values into pages of 8 bits, keys and queries normed and rotated on the way, and rows read back.
 //
 // A head's entries lie eight to a lane in a group of G lanes, so that four lanes hold a block of 32 and the group a head.  A wave
-// takes a token, its groups the token's heads one after the other: place, angles and weights are looked up once.
+// takes a token, its groups the token's heads one after the other, values, keys, queries: place, angles and weights are looked up once.
 //
 // Rounding to 8 bits is the only rounding that may show, so what leads there is exact or in 64 bits, which the vector units do at
 // the rate of 32: with weight w, angle (c, s) and partner x' (weight w') an entry is r (x w c +- x' w' s), where w c and w' s are
@@ -21,7 +21,7 @@ struct PackedAppendArgs {
     const void *k_norm, *q_norm;
     const float *cos, *sin;
     const int32_t *positions, *q_start, *kv_len, *table;
-    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, head_dim, rot, n_pos, interleaved, norm_f32, slices;
+    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, head_dim, rot, n_pos, interleaved, norm_f32, slices, kinds;
     double eps, inv_dim;
 };
 
@@ -96,7 +96,7 @@ __device__ __forceinline__ double sum_of_head(double x) {
 // The upper 21 bits of a double as a float, the last one set where a bit below is.
 __device__ __forceinline__ float to_odd(double x) {
     const u64 b = (u64)__double_as_longlong(x);
-    const u32 hi = (u32)(b >> 32) | ((u32)b ? 1u : 0u);
+    const u32 hi = (u32)(b >> 32) | min((u32)b, 1u);
     return (float)__longlong_as_double((long long)((u64)hi << 32));
 }
 // 1 / sqrt(x) to the last bits of a double: the hardware's value and a step of third order.
@@ -137,112 +137,204 @@ __device__ __forceinline__ uint2 pack8(const float *x, u32 &power) {
     return r;
 }
 
+// The arguments, read anew: held all at once they would take more scalar registers than there are, and go through vector registers
+// lane by lane.
+typedef const __attribute__((address_space(4))) PackedAppendArgs LateArgs;
+__device__ __forceinline__ LateArgs *late_args() {
+    LateArgs *p = (LateArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// A job: a token, and of its values (kind 0), keys (1) and queries (2) all or, where there are few tokens, one.
 template <class T, int FORM, int G>
 __global__ __launch_bounds__(256) void packed_append_kernel(PackedAppendArgs a) {
     constexpr u32 GROUPS = 64 / G;
     __shared__ __attribute__((aligned(16))) float lds[256 * 8];
+    __shared__ __attribute__((aligned(16))) float weights[2][G * 8];  // of keys, of queries
     const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const u64 job = (u64)blockIdx.x * 4 + wave;
-    const u32 t = (u32)(job / a.slices), slice = (u32)(job % a.slices);
-    if (t >= a.n_tokens) return;
-    const TokenPlace at = place_of(a, t);
-    const u32 group = lane / G, c = lane % G * 8, half = a.rot / 2;
-    const bool live = c < a.head_dim;
-    float *own = lds + (threadIdx.x - lane % G) * 8;  // the head's entries
-    const i64 angle_at = a.positions ? (i64)a.positions[t] : at.pos;
-    const bool angle = angle_at >= 0 && angle_at < (i64)a.n_pos;
-    u32 partner[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const u32 j = c + i;
-        partner[i] = !live || j >= a.rot ? 0 : a.interleaved ? j ^ 1 : j < half ? j + half : j - half;
+    for (u32 k = 0; k < 2; ++k) {
+        const void *norm = k ? a.q_norm : a.k_norm;
+        for (u32 i = threadIdx.x; i < G * 8; i += 256)
+            weights[k][i] = !norm || i >= a.head_dim ? 1.0f : a.norm_f32 ? ((const float *)norm)[i] : (float)((const T *)norm)[i];
     }
-    double A[8], B[8];  // of a normed and rotated entry and of its partner: weight times cosine, weight times +-sine
-    u32 kind = 0;       // what they belong to: 1 keys, 2 queries
-    const u32 all = 2 * a.kv_heads + a.heads, step = a.slices * GROUPS;
-    for (u32 h = slice * GROUPS + group; h < all; h += step) {
-        const bool is_k = h < a.kv_heads, is_v = !is_k && h < 2 * a.kv_heads;
-        const u32 head = is_k ? h : is_v ? h - a.kv_heads : h - 2 * a.kv_heads;
-        if ((is_k || is_v) && at.page < 0) continue;
-        const T *src = is_k   ? (const T *)a.k + (i64)t * a.ks[0] + head * a.ks[1]
-                       : is_v ? (const T *)a.v + (i64)t * a.vs[0] + head * a.vs[1]
-                              : (const T *)a.q + (i64)t * a.qs[0] + head * a.qs[1];
-        Pack<T, 8> in{};
-        if (live) in = load_pack<8>(src + c);
-        float x[8];
+    __syncthreads();
+    const u32 t = blockIdx.x * 4 + wave, kinds = a.kinds, only = blockIdx.y % kinds, slice = blockIdx.y / kinds;
+    if (t >= a.n_tokens) return;
+    const u32 first = slice * GROUPS + lane / G, step = a.slices * GROUPS;  // heads of the group
+    const u32 c = lane % G * 8, dim = a.head_dim, rot = a.rot, half = rot / 2;
+    const bool live = c < dim, interleaved = a.interleaved;
+    const u32 at_c = live ? c : 0;
+    const TokenPlace at = place_of(a, t);
+    float *own = lds + (threadIdx.x - lane % G) * 8;  // the head's entries
+
+    // use(head, entries) for the group's heads, the next one's entries under way
+    auto each_head = [&](const void *rows, i64 stride0, i64 stride1, u32 heads, auto use) {
+        const T *src = (const T *)rows + (i64)t * stride0 + at_c;
+        Pack<T, 8> next{};
+        if (first < heads) next = load_pack<8>(src + first * stride1);
+        for (u32 h = first; h < heads; h += step) {
+            const Pack<T, 8> in = next;
+            next = load_pack<8>(src + min(h + step, heads - 1) * stride1);
+            float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)in.v[i];
-        const void *norm = is_k ? a.k_norm : is_v ? nullptr : a.q_norm;
-        const bool turn = !is_v && a.rot;
-        if (norm || turn) {
-            const u32 want = is_k ? 1 : 2;
-            if (kind != want) {
-                kind = want;
+            for (int i = 0; i < 8; ++i) x[i] = live ? (float)in.v[i] : 0.0f;
+            use(h, x);
+        }
+    };
+    auto store_codes = [&](const float *x, unsigned char *codes, unsigned char *powers) {
+        u32 power;
+        const uint2 packed = pack8<FORM>(x, power);
+        if (live) {
+            __builtin_memcpy(codes + c, &packed, 8);
+            if (c % PACK_BLOCK == 0) powers[c / PACK_BLOCK] = (unsigned char)power;
+        }
+    };
+    if (at.page >= 0 && (kinds == 1 || only == 0)) {
+        LateArgs *p = late_args();
+        unsigned char *codes = p->pv + at.page * p->pvs[0] + (i64)at.row * p->pvs[2], *powers = p->zv + at.page * p->zvs[0] + (i64)at.row * p->zvs[2];
+        const i64 sc = p->pvs[1], sz = p->zvs[1];
+        each_head(p->v, p->vs[0], p->vs[1], p->kv_heads, [&](u32 h, const float *x) { store_codes(x, codes + h * sc, powers + h * sz); });
+    }
+    if (kinds > 1 && only == 0) return;
+
+    // Keys and queries: A of an entry is its weight times the cosine, B its partner's weight times +-sine.
+    const bool by_four = !interleaved && half % 4 == 0, part = rot < dim;
+    auto partner = [&](u32 j) { return j >= rot ? j : interleaved ? j ^ 1 : j < half ? j + half : j - half; };
+    float cs[8], sn[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const u32 j = c + i, jp = partner[i];
-                    double w = 1.0, wp = 1.0;
-                    if (norm && live) {
-                        w = a.norm_f32 ? (double)((const float *)norm)[j] : (double)(float)((const T *)norm)[j];
-                        wp = a.norm_f32 ? (double)((const float *)norm)[jp] : (double)(float)((const T *)norm)[jp];
-                    }
-                    A[i] = w;
-                    B[i] = 0.0;
-                    if (live && j < a.rot) {
-                        const u32 f = a.interleaved ? j / 2 : j < half ? j : j - half;
-                        const bool minus = a.interleaved ? !(j & 1) : j < half;
-                        const double cs = angle ? (double)a.cos[angle_at * half + f] : __builtin_nan(""), sn = angle ? (double)a.sin[angle_at * half + f] : 0.0;
-                        A[i] = w * cs;
-                        B[i] = wp * (minus ? -sn : sn);
-                    }
-                }
-            }
-            double r = 1.0;
-            if (norm) {
-                double ss = 0.0;
+    for (int i = 0; i < 8; ++i) cs[i] = 1.0f, sn[i] = 0.0f;
+    if (rot) {
+        LateArgs *p = late_args();
+        const i64 angle_at = p->positions ? (i64)p->positions[t] : at.pos;
+        const bool angle = angle_at >= 0 && angle_at < (i64)p->n_pos;
+        const float *cos = p->cos + (angle ? angle_at * half : 0), *sin = p->sin + (angle ? angle_at * half : 0);
+        const u32 f = interleaved ? c / 2 : c < half ? c : c - half;
+        if (angle && c + 8 <= rot && (interleaved || half % 8 == 0)) {
+            if (interleaved) {
+                const Pack<float, 4> u = load_pack<4>(cos + f), v = load_pack<4>(sin + f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)x[i], (double)x[i], ss);
-                r = rsqrt_of(__builtin_fma(sum_of_head<G>(ss), a.inv_dim, a.eps));
-            }
-            float p[8];
-            if (turn) {
-                *(float4 *)(own + c) = make_float4(x[0], x[1], x[2], x[3]);
-                *(float4 *)(own + c + 4) = make_float4(x[4], x[5], x[6], x[7]);
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = c + i < a.rot ? own[partner[i]] : 0.0f;
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+                for (int i = 0; i < 8; ++i) cs[i] = u.v[i / 2], sn[i] = i % 2 ? v.v[i / 2] : -v.v[i / 2];
             } else {
+                const Pack<float, 8> u = load_pack<8>(cos + f), v = load_pack<8>(sin + f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = 0.0f;
+                for (int i = 0; i < 8; ++i) cs[i] = u.v[i], sn[i] = c < half ? -v.v[i] : v.v[i];
+            }
+        } else if (p->n_pos) {
+            // every lane loads, some for nothing: a branch around a load would be a wait for it
+            float u[8], v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const u32 j = c + i, f = j >= rot ? 0 : interleaved ? j / 2 : j < half ? j : j - half;
+                u[i] = cos[f];
+                v[i] = sin[f];
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const double y = __builtin_fma((double)p[i], B[i], (double)x[i] * A[i]) * r;
-                x[i] = sizeof(T) == 4 && !is_k ? (float)y : to_odd(y);
+                const u32 j = c + i;
+                const bool minus = interleaved ? !(j & 1) : j < half;
+                if (j < rot) {
+                    cs[i] = angle ? u[i] : __builtin_nanf("");
+                    sn[i] = angle ? (minus ? -v[i] : v[i]) : 0.0f;
+                }
             }
-        }
-        if (!live)
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-        if (is_k || is_v) {
-            u32 power;
-            const uint2 codes = pack8<FORM>(x, power);
-            if (!live) continue;
-            unsigned char *dst = is_k ? a.pk + at.page * a.pks[0] + head * a.pks[1] + (i64)at.row * a.pks[2]
-                                      : a.pv + at.page * a.pvs[0] + head * a.pvs[1] + (i64)at.row * a.pvs[2];
-            unsigned char *z = is_k ? a.zk + at.page * a.zks[0] + head * a.zks[1] + (i64)at.row * a.zks[2]
-                                    : a.zv + at.page * a.zvs[0] + head * a.zvs[1] + (i64)at.row * a.zvs[2];
-            __builtin_memcpy(dst + c, &codes, 8);
-            if (c % PACK_BLOCK == 0) z[c / PACK_BLOCK] = (unsigned char)power;
-        } else if (live) {
-            Pack<T, 8> out;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out.v[i] = (T)x[i];
-            store_pack<8>((T *)a.qo + (i64)t * a.qos[0] + head * a.qos[1] + c, out);
+            for (int i = 0; i < 8; ++i) cs[i] = c + i < rot ? __builtin_nanf("") : 1.0f;
         }
+    }
+    // where the partners of a head's entries stand in LDS
+    const u32 pa = live ? partner(c) : c, pb = live ? partner(c + 4) : c + 4;
+    auto partners_of = [&](const float *x, float *p) {
+        if (by_four) {
+            const float4 u = *(const float4 *)(x + pa), v = *(const float4 *)(x + pb);
+            p[0] = u.x, p[1] = u.y, p[2] = u.z, p[3] = u.w;
+            p[4] = v.x, p[5] = v.y, p[6] = v.z, p[7] = v.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = x[live ? partner(c + i) : c];
+        }
+    };
+    auto partners = [&](const float *x, float *p) {
+        if (interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = x[i ^ 1];
+        } else {
+            *(float4 *)(own + c) = make_float4(x[0], x[1], x[2], x[3]);
+            *(float4 *)(own + c + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            partners_of(own, p);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (part)  // those that are not rotated have none, whatever stands in their place
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = c + i < rot ? p[i] : 0.0f;
+    };
+    auto factors = [&](const float *w, double *A, double *B) {
+        float wp[8];
+        partners_of(w, wp);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) A[i] = (double)cs[i] * (double)w[c + i], B[i] = (double)sn[i] * (double)wp[i];
+    };
+    const double eps = a.eps, inv_dim = a.inv_dim;
+    auto turned = [&](bool norm, const double *A, const double *B, const float *x, double *y) {
+        double r = 1.0;
+        if (norm) {
+            double ss = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = __builtin_fma((double)x[i], (double)x[i], ss);
+            r = rsqrt_of(__builtin_fma(sum_of_head<G>(ss), inv_dim, eps));
+        }
+        if (rot) {
+            float p[8];
+            partners(x, p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = __builtin_fma((double)p[i], B[i], (double)x[i] * A[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = (double)x[i] * A[i];
+        }
+        if (norm)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] *= r;
+    };
+    double A[8], B[8];
+    if (at.page >= 0 && (kinds == 1 || only == 1)) {
+        LateArgs *p = late_args();
+        const bool norm = p->k_norm, plain = !norm && !rot;
+        factors(weights[0], A, B);
+        unsigned char *codes = p->pk + at.page * p->pks[0] + (i64)at.row * p->pks[2], *powers = p->zk + at.page * p->zks[0] + (i64)at.row * p->zks[2];
+        const i64 sc = p->pks[1], sz = p->zks[1];
+        each_head(p->k, p->ks[0], p->ks[1], p->kv_heads, [&](u32 h, float *x) {
+            if (!plain) {
+                double y[8];
+                turned(norm, A, B, x, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = to_odd(y[i]);
+            }
+            store_codes(x, codes + h * sc, powers + h * sz);
+        });
+    }
+    if (kinds == 1 || only == 2) {
+        LateArgs *p = late_args();
+        const bool norm = p->q_norm, plain = !norm && !rot;
+        factors(weights[1], A, B);
+        T *out = (T *)p->qo + (i64)t * p->qos[0] + c;
+        const i64 so = p->qos[1];
+        each_head(p->q, p->qs[0], p->qs[1], p->heads, [&](u32 h, float *x) {
+            Pack<T, 8> y8;
+            if (!plain) {
+                double y[8];
+                turned(norm, A, B, x, y);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y8.v[i] = (T)x[i];
+            if (live) store_pack<8>(out + h * so, y8);
+        });
     }
 }
 
@@ -291,9 +383,9 @@ static u32 slices_of(u32 n_tokens, u32 turns) { return std::max(1u, std::min(tur
 
 template <class T, int FORM, int G>
 static int launch_packed_append(PackedAppendArgs a, hipStream_t st) {
-    a.slices = slices_of(a.n_tokens, (2 * a.kv_heads + a.heads + 64 / G - 1) / (64 / G));
-    const u64 blocks = ((u64)a.n_tokens * a.slices + 3) / 4;
-    hipLaunchKernelGGL((packed_append_kernel<T, FORM, G>), dim3((u32)blocks), dim3(256), 0, st, a);
+    a.slices = slices_of(a.n_tokens, (std::max(a.kv_heads, a.heads) + 64 / G - 1) / (64 / G));
+    a.kinds = a.n_tokens * a.slices <= 2048 ? 3 : 1;
+    hipLaunchKernelGGL((packed_append_kernel<T, FORM, G>), dim3((a.n_tokens + 3) / 4, a.slices * a.kinds), dim3(256), 0, st, a);
     CKKS_LAUNCH_CHECK("packed_append_kernel");
     return CKKS_OK;
 }

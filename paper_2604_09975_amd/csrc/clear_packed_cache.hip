@@ -148,7 +148,7 @@ __device__ __forceinline__ LateArgs *late_args() {
 
 // A job: a token, and of its values (kind 0), keys (1) and queries (2) all or, where there are few tokens, one.
 template <class T, int FORM, int G>
-__global__ __launch_bounds__(256) void packed_append_kernel(PackedAppendArgs a) {
+__global__ __launch_bounds__(256, 4) void packed_append_kernel(PackedAppendArgs a) {
     constexpr u32 GROUPS = 64 / G;
     __shared__ __attribute__((aligned(16))) float lds[256 * 8];
     __shared__ __attribute__((aligned(16))) float weights[2][G * 8];  // of keys, of queries
@@ -210,8 +210,9 @@ __global__ __launch_bounds__(256) void packed_append_kernel(PackedAppendArgs a) 
         const bool angle = angle_at >= 0 && angle_at < (i64)p->n_pos;
         const float *cos = p->cos + (angle ? angle_at * half : 0), *sin = p->sin + (angle ? angle_at * half : 0);
         const u32 f = interleaved ? c / 2 : c < half ? c : c - half;
-        if (angle && c + 8 <= rot && (interleaved || half % 8 == 0)) {
-            if (interleaved) {
+        if (angle && rot % 8 == 0 && (interleaved || half % 8 == 0)) {  // all of a lane's entries are rotated, or none
+            if (c >= rot) {
+            } else if (interleaved) {
                 const Pack<float, 4> u = load_pack<4>(cos + f), v = load_pack<4>(sin + f);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) cs[i] = u.v[i / 2], sn[i] = i % 2 ? v.v[i / 2] : -v.v[i / 2];

@@ -26,7 +26,7 @@ using namespace ckks;
 
 static AttendSizes sizes(const ckks_clear_attend_t &p) {
     const ckks_clear_pages_t &g = p.pages;
-    return {p.batch, p.heads, g.kv_heads, g.head_dim, g.page_size, g.dtype, p.flags, p.window, 2.0 * g.head_dim * clear_dtype_bytes(g.dtype)};
+    return {p.batch, p.heads, g.kv_heads, g.head_dim, g.page_size, g.dtype, p.flags, p.window, 2.0 * g.head_dim * clear_dtype_bytes(g.dtype), nullptr};
 }
 
 extern "C" {

@@ -919,7 +919,8 @@ struct AttendPlan {
 struct AttendSizes {
     const ckks_clear_batch_t &batch;
     u32 heads, kv_heads, head_dim, page_size, dtype, flags, window;
-    double key_bytes;  // of a key and its value in the cache
+    double key_bytes;             // of a key and its value in the cache
+    const AttendForm *thin = nullptr;  // a form more
 };
 static bool plan_attend(const AttendSizes &p, AttendPlan &n) {
     const AttendSizes &g = p;
@@ -943,8 +944,8 @@ static bool plan_attend(const AttendSizes &p, AttendPlan &n) {
     const double key_bytes = p.key_bytes, all = seqs * g.kv_heads * keys * key_bytes;
     double best = 0;
     n.splits = 0;
-    for (u32 f = 0; f < count; ++f) {
-        const AttendForm &form = forms[f];
+    for (u32 f = 0; f < count + (p.thin != nullptr); ++f) {
+        const AttendForm &form = f < count ? forms[f] : *p.thin;
         const double blocks = (seqs ? seqs * std::ceil(per_seq / form.rows) : 1) * g.kv_heads;
         const bool may_split = (u64)b.n_tokens * p.heads < 1u << 31;  // the joining kernel's grid
         const double most = !may_split ? 1.0 : std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));
@@ -978,22 +979,25 @@ static bool plan_attend(const AttendSizes &p, AttendPlan &n) {
     return true;
 }
 
+template <class T, int ROWS, int TK>
+static int launch_join(const AttendArgs &a, u32 lanes, hipStream_t st) {
+    if (a.splits > 1) {
+        const u64 rows = (u64)a.n_tokens * a.heads;
+        if (a.splits <= 8)
+            hipLaunchKernelGGL((attend_join_kernel<T, ROWS, TK, 1>), dim3((u32)((rows + 3) / 4)), dim3(256), 0, st, a, lanes);
+        else if (a.splits <= 32)
+            hipLaunchKernelGGL((attend_join_kernel<T, ROWS, TK, 4>), dim3((u32)rows), dim3(256), 0, st, a, lanes);
+        else
+            hipLaunchKernelGGL((attend_join_kernel<T, ROWS, TK, 16>), dim3((u32)rows), dim3(1024), 0, st, a, lanes);
+        CKKS_LAUNCH_CHECK("attend_join_kernel");
+    }
+    return CKKS_OK;
+}
 template <class T, int FORM, int DP, int RW, int KW, int TK, int OCC>
 static int launch_attend(const typename Stored<T, FORM>::args &a, hipStream_t st) {
     hipLaunchKernelGGL((attend_kernel<T, FORM, DP, RW, KW, TK, OCC>), dim3(a.kv_heads * a.splits * a.tiles), dim3(64 * RW * KW), 0, st, a);
     CKKS_LAUNCH_CHECK("attend_kernel");
-    if (a.splits > 1) {
-        const u64 rows = (u64)a.n_tokens * a.heads;
-        const u32 lanes = DP / 4;
-        if (a.splits <= 8)
-            hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK, 1>), dim3((u32)((rows + 3) / 4)), dim3(256), 0, st, (const AttendArgs &)a, lanes);
-        else if (a.splits <= 32)
-            hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK, 4>), dim3((u32)rows), dim3(256), 0, st, (const AttendArgs &)a, lanes);
-        else
-            hipLaunchKernelGGL((attend_join_kernel<T, 32 * RW, TK, 16>), dim3((u32)rows), dim3(1024), 0, st, (const AttendArgs &)a, lanes);
-        CKKS_LAUNCH_CHECK("attend_join_kernel");
-    }
-    return CKKS_OK;
+    return launch_join<T, 32 * RW, TK>(a, DP / 4, st);
 }
 template <class T, int FORM>
 static int launch_attend(const typename Stored<T, FORM>::args &a, const AttendPlan &n, hipStream_t st) {

@@ -48,7 +48,8 @@ __device__ __forceinline__ float row_sum(float x) {
 //   scores: lane l has row l % 16, keys 4 (l / 16) + i and 16 more;
 //   values: expanded with their powers on the way into LDS, read back by columns for the very keys that the lane has weights of.
 // Bound by memory: what a wave does with a tile's 8 KB takes a quarter of the time that its share of the memory's rate takes.
-template <class T, int FORM, int DP, int KW, int OCC>
+// WHOLE: pages hold whole tiles.
+template <class T, int FORM, int DP, bool WHOLE, int KW, int AHEAD, int OCC>
 __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendArgs a) {
     typedef typename Thin<T>::type C;
     typedef typename Frag<C>::type frag;
@@ -116,29 +117,29 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
     const unsigned char *kp = (const unsigned char *)a.k + (i64)kv_head * a.ks[1], *vp = (const unsigned char *)a.v + (i64)kv_head * a.vs[1];
     const unsigned char *kzp = a.kz + (i64)kv_head * a.kzs[1] + k_block, *vzp = a.vz + (i64)kv_head * a.vzs[1] + v_block;
     const int32_t *table = a.table + (i64)r.seq * a.ts;
-    const bool whole = a.page_size % TK == 0;
+    // (a page lies within 2^31 bytes: check_cache)
+    const u32 ks2 = (u32)a.ks[2], vs2 = (u32)a.vs[2], kzs2 = (u32)a.kzs[2], vzs2 = (u32)a.vzs[2];
+    const u32 k_lane = key_row * ks2 + quarter * QUARTER, v_lane = fetch_row * vs2 + (piece_ok ? piece * 16 : 0), kz_lane = key_row * kzs2, vz_lane = fetch_row * vzs2;
+    const bool full = a.head_dim == DP;
+    constexpr int NK = WHOLE ? 1 : 2, NV = WHOLE ? 1 : PASSES;
     struct Place {
-        u32 k_page[2], k_row[2], v_page[PASSES], v_row[PASSES];  // of each row
-        u32 tile_page, tile_row;                                 // of the tile, where pages hold whole tiles
+        u32 k_page[NK], k_row[NK], v_page[NV], v_row[NV];  // of each row; of the tile, where pages hold whole tiles
     };
     auto look_up = [&](u32 tile) {
         Place at;
         const u32 j0 = (r.tile0 + tile) * TK;
-        if (whole) {
-            const u32 j = min(j0, ((u32)r.kv - 1) / TK * TK), n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
-            at.tile_page = (u32)table[n];
-            at.tile_row = j - n * a.page_size;
+        auto one = [&](u32 j, u32 &page, u32 &row) {
+            const u32 n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
+            page = (u32)table[n];
+            row = j - n * a.page_size;
+        };
+        if constexpr (WHOLE) {
+            one(min(j0, ((u32)r.kv - 1) / TK * TK), at.k_page[0], at.k_row[0]);
         } else {
-            auto one = [&](u32 j, u32 &page, u32 &row) {
-                j = min(j, (u32)r.kv - 1);
-                const u32 n = __umulhi(2 * j, a.page_mul) >> a.page_shift;
-                page = (u32)table[n];
-                row = j - n * a.page_size;
-            };
 #pragma unroll
-            for (int u = 0; u < 2; ++u) one(j0 + 16 * u + key_row, at.k_page[u], at.k_row[u]);
+            for (int u = 0; u < 2; ++u) one(min(j0 + 16 * u + key_row, (u32)r.kv - 1), at.k_page[u], at.k_row[u]);
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) one(j0 + p * PASS + fetch_row, at.v_page[p], at.v_row[p]);
+            for (int p = 0; p < PASSES; ++p) one(min(j0 + p * PASS + fetch_row, (u32)r.kv - 1), at.v_page[p], at.v_row[p]);
         }
         return at;
     };
@@ -151,30 +152,38 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
         Tile x;
         x.none = 0;
         const u32 j0 = (r.tile0 + tile) * TK;
-        auto k_from = [&](int u, u32 page, u32 row, bool ok) {
-            if (!ok) x.none |= 1u << u;
-            const unsigned char *k = kp + ((u64)page * (u32)a.ks[0] + row * (u32)a.ks[2]);
+        // from a base and the lane's place
+        auto k_from = [&](int u, const unsigned char *k, u32 lane, const unsigned char *kz, u32 z_lane) {
 #pragma unroll
-            for (int h = 0; h < KP; ++h) __builtin_memcpy(&x.k[u][h], k + (k_ok[h] ? quarter * QUARTER + h * 16 : 0), 16);
-            x.kz[u] = kzp[(u64)page * (u32)a.kzs[0] + row * (u32)a.kzs[2]];
+            for (int h = 0; h < KP; ++h) __builtin_memcpy(&x.k[u][h], k + (lane + (full || k_ok[h] ? h * 16 : 0u - quarter * QUARTER)), 16);
+            x.kz[u] = kz[z_lane];
         };
-        auto v_from = [&](int p, u32 page, u32 row, bool ok) {
-            if (!ok) x.none |= 4u << p;
-            __builtin_memcpy(&x.v[p], vp + ((u64)page * (u32)a.vs[0] + (row * (u32)a.vs[2] + (piece_ok ? piece * 16 : 0))), 16);
-            x.vz[p] = vzp[(u64)page * (u32)a.vzs[0] + row * (u32)a.vzs[2]];
+        auto v_from = [&](int p, const unsigned char *v, u32 lane, const unsigned char *vz, u32 z_lane) {
+            __builtin_memcpy(&x.v[p], v + lane, 16);
+            x.vz[p] = vz[z_lane];
         };
-        if (whole) {
-            const bool ok = at.tile_page < a.n_pages;
-            const u32 page = ok ? at.tile_page : 0;
+        if constexpr (WHOLE) {
+            const u32 page = at.k_page[0] < a.n_pages ? at.k_page[0] : 0, row = at.k_row[0];
+            if (at.k_page[0] >= a.n_pages) x.none = ~0u;
+            const unsigned char *k = kp + ((u64)page * (u32)a.ks[0] + row * ks2), *kz = kzp + ((u64)page * (u32)a.kzs[0] + row * kzs2);
+            const unsigned char *v = vp + ((u64)page * (u32)a.vs[0] + row * vs2), *vz = vzp + ((u64)page * (u32)a.vzs[0] + row * vzs2);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) k_from(u, page, at.tile_row + 16 * u + key_row, ok);
+            for (int u = 0; u < 2; ++u) k_from(u, k + 16 * u * ks2, k_lane, kz + 16 * u * kzs2, kz_lane);
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) v_from(p, page, at.tile_row + p * PASS + fetch_row, ok);
+            for (int p = 0; p < PASSES; ++p) v_from(p, v + p * PASS * vs2, v_lane, vz + p * PASS * vzs2, vz_lane);
         } else {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) k_from(u, at.k_page[u] < a.n_pages ? at.k_page[u] : 0, at.k_row[u], at.k_page[u] < a.n_pages);
+            for (int u = 0; u < 2; ++u) {
+                const u32 page = at.k_page[u] < a.n_pages ? at.k_page[u] : 0, row = at.k_row[u];
+                if (at.k_page[u] >= a.n_pages) x.none |= 1u << u;
+                k_from(u, kp + (u64)page * (u32)a.ks[0], row * ks2 + quarter * QUARTER, kzp + (u64)page * (u32)a.kzs[0], row * kzs2);
+            }
 #pragma unroll
-            for (int p = 0; p < PASSES; ++p) v_from(p, at.v_page[p] < a.n_pages ? at.v_page[p] : 0, at.v_row[p], at.v_page[p] < a.n_pages);
+            for (int p = 0; p < PASSES; ++p) {
+                const u32 page = at.v_page[p] < a.n_pages ? at.v_page[p] : 0, row = at.v_row[p];
+                if (at.v_page[p] >= a.n_pages) x.none |= 4u << p;
+                v_from(p, vp + (u64)page * (u32)a.vs[0], row * vs2 + (piece_ok ? piece * 16 : 0), vzp + (u64)page * (u32)a.vzs[0], row * vzs2);
+            }
         }
         if (j0 + TK > (u32)r.kv) {
 #pragma unroll
@@ -198,7 +207,14 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
     u32 odd = 0;
     C *vb = (C *)lds + kw * TK * VS;
 
+    auto k_power = [&](float power, int h) { return full || k_ok[h] ? power : 1.0f; };
     auto score = [&](Tile &x) {
+        if (!full)  // what a lane has beyond the head
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int h = 0; h < KP; ++h)
+                    if (!k_ok[h]) x.k[u][h] = make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if (__any(x.none & 3u))
@@ -214,11 +230,8 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
             for (int d = 0; d < STEPS; ++d) {
                 C k[8];
                 const uint4 y = x.k[u][d / 2];
-                unpack4<C, FORM>(d % 2 ? y.z : y.x, power, k);
-                unpack4<C, FORM>(d % 2 ? y.w : y.y, power, k + 4);
-                if (!k_ok[d / 2])
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) k[i] = (C)0.0f;
+                unpack4<C, FORM>(d % 2 ? y.z : y.x, k_power(power, d / 2), k);
+                unpack4<C, FORM>(d % 2 ? y.w : y.y, k_power(power, d / 2), k + 4);
                 frag f;
                 __builtin_memcpy(&f, k, 16);
 #pragma unroll
@@ -308,23 +321,33 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
         }
     };
 
+    // AHEAD tiles of the wave are under way, the places of the one behind them looked up.
     if (first + kw < last) {
+        Tile x[AHEAD];
         Place at = look_up(first + kw);
-        Tile x = fetch(first + kw, at);
-        at = look_up(first + kw + KW);
-        for (u32 i = first + kw; i < last; i += KW) {
-            put_v(i, x);
-            score(x);
-            if (i + KW < last) {
-                x = fetch(i + KW, at);
-                at = look_up(i + 2 * KW);
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            x[n] = fetch(first + kw + n * KW, at);
+            at = look_up(first + kw + (n + 1) * KW);
+        }
+        for (u32 i = first + kw; i < last; i += AHEAD * KW) {
+#pragma unroll
+            for (int n = 0; n < AHEAD; ++n) {
+                const u32 tile = i + n * KW;
+                if (tile >= last) break;
+                put_v(tile, x[n]);
+                score(x[n]);
+                if (tile + AHEAD * KW < last) {
+                    x[n] = fetch(tile + AHEAD * KW, at);
+                    at = look_up(tile + (AHEAD + 1) * KW);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                soften(tile);
+                gather();
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            soften(i);
-            gather();
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
         }
     }
     l = row_sum(l);
@@ -424,7 +447,12 @@ static AttendSizes sizes(const ckks_clear_packed_attend_t &p) {
 }
 template <class T, int FORM, int DP>
 static int launch_thin(const PackedAttendArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((attend_thin_kernel<T, FORM, DP, 4, sizeof(T) == 4 && DP == 128 ? 2 : 3>), dim3(a.kv_heads * a.splits * a.tiles), dim3(256), 0, st, a);
+    constexpr int OCC = sizeof(T) == 4 && DP == 128 ? 2 : 3;
+    const dim3 grid(a.kv_heads * a.splits * a.tiles);
+    if (a.page_size % 32)
+        hipLaunchKernelGGL((attend_thin_kernel<T, FORM, DP, false, 4, 1, OCC>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((attend_thin_kernel<T, FORM, DP, true, 4, 1, OCC>), grid, dim3(256), 0, st, a);
     CKKS_LAUNCH_CHECK("attend_thin_kernel");
     return launch_join<T, 16, 32>(a, DP / 4, st);
 }

@@ -946,6 +946,7 @@ static bool plan_attend(const AttendSizes &p, AttendPlan &n) {
     n.splits = 0;
     for (u32 f = 0; f < count + (p.thin != nullptr); ++f) {
         const AttendForm &form = f < count ? forms[f] : *p.thin;
+        if (p.thin && f < count && (f32 || form.waves_rows == 1)) continue;  // what it takes the place of
         const double blocks = (seqs ? seqs * std::ceil(per_seq / form.rows) : 1) * g.kv_heads;
         const bool may_split = (u64)b.n_tokens * p.heads < 1u << 31;  // the joining kernel's grid
         const double most = !may_split ? 1.0 : std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));

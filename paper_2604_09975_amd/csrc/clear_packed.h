@@ -9,17 +9,21 @@ namespace ckks {
 constexpr int PLAIN = 0, E4M3 = CKKS_CLEAR_E4M3, I8 = CKKS_CLEAR_I8;  // forms of a page
 constexpr u32 PACK_BLOCK = 32;                                        // entries that share a power of two
 
-// 2^(z - 127); NaN for 255, which the conversions below pass on.  (The hardware's scaled conversions, exact for every code and power,
-// read the exponent field of a float only, 255 of which is their NaN too; what the float for 0 holds is the denormal 2^-127.)
-__device__ __forceinline__ float power_of(u32 z) { return __uint_as_float(z == 0 ? 0x00400000u : z == 255 ? 0x7fc00000u : z << 23); }
+// 2^(z - 127), NaN for 255, as the conversions below take it: those of the hardware, exact for every code and power, read the exponent
+// field of a float, 255 of which is their NaN; to multiply by, 0 is the denormal 2^-127.
+template <int FORM>
+__device__ __forceinline__ float power_of(u32 z) {
+    if (FORM == E4M3) return __uint_as_float(z << 23);
+    return __uint_as_float(z == 0 ? 0x00400000u : z == 255 ? 0x7fc00000u : z << 23);
+}
 
 // The value of one code.
 template <int FORM>
 __device__ __forceinline__ float unpack(u32 code, u32 z) {
     if constexpr (FORM == E4M3)
-        return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code, power_of(z), false)[0];
+        return __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code, power_of<FORM>(z), false)[0];
     else
-        return (float)(signed char)code * power_of(z);
+        return (float)(signed char)code * power_of<FORM>(z);
 }
 
 // Four codes of one block as T.
@@ -45,7 +49,7 @@ __device__ __forceinline__ void unpack4(u32 codes, float power, T *out) {
 template <class T, int FORM, class P>
 __device__ __forceinline__ uint4 unpack_piece(const P &x, u32 z) {
     T v[16 / sizeof(T)];
-    const float power = power_of(z);
+    const float power = power_of<FORM>(z);
     if constexpr (sizeof(P) == 8) {
         unpack4<T, FORM>(x.x, power, v);
         unpack4<T, FORM>(x.y, power, v + 4);

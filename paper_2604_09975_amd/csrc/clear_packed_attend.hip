@@ -223,7 +223,7 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
                     for (int h = 0; h < KP; ++h) x.k[u][h] = make_uint4(0, 0, 0, 0);
                     x.kz[u] = 0;
                 }
-            const float power = power_of(x.kz[u]);
+            const float power = power_of<FORM>(x.kz[u]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[u][i] = 0.0f;
 #pragma unroll
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             C v[16];
-            const float power = power_of(x.vz[p]);
+            const float power = power_of<FORM>(x.vz[p]);
             unpack4<C, FORM>(x.v[p].x, power, v);
             unpack4<C, FORM>(x.v[p].y, power, v + 4);
             unpack4<C, FORM>(x.v[p].z, power, v + 8);

@@ -372,8 +372,8 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedReadArgs a) {
             power = z[c / PACK_BLOCK];
         }
         Pack<T, 8> out;
-        unpack4<T, FORM>(codes.x, power_of(power), out.v);
-        unpack4<T, FORM>(codes.y, power_of(power), out.v + 4);
+        unpack4<T, FORM>(codes.x, power_of<FORM>(power), out.v);
+        unpack4<T, FORM>(codes.y, power_of<FORM>(power), out.v + 4);
         T *dst = is_k ? (T *)a.ko + (i64)t * a.kos[0] + head * a.kos[1] : (T *)a.vo + (i64)t * a.vos[0] + head * a.vos[1];
         store_pack<8>(dst + c, out);
     }

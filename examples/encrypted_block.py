@@ -3,7 +3,8 @@
 The server holds the plaintext weights of the QKV and the output projection and sees ciphertexts only.  The key holder decrypts
 between the two and does the rest in the clear on the same device: layer norm, the paged key / value cache with the position
 rotation, attention of a chunk of tokens over it, and the rules on the logits.  A prompt goes through in chunks of one segment,
-the new tokens one at a time through the same calls.  `tune` trains the parameters of the last layer norm, which the key holder
+the new tokens one at a time through the same calls.  With `packed` the cache takes a byte for each entry, and with `draw` the next token
+is drawn instead of taken as the largest.  `tune` trains the parameters of the last layer norm, which the key holder
 can do alone: they meet no ciphertext.
 
 Random weights; a ring of 2^13 (three 45-bit primes, one special prime), so that it runs in seconds.
@@ -52,9 +53,9 @@ class Projection:
 
 
 class Block:
-    """Embedding, layer norm, attention, residual, layer norm, logits."""
+    """Embedding, layer norm, attention, residual, layer norm, logits.  packed: float8_e4m3fn or int8 for a cache of 8 bits."""
 
-    def __init__(self, seed=1, max_tokens=96):
+    def __init__(self, seed=1, max_tokens=96, packed=None):
         r = np.random.default_rng(seed)
         P = B.ckks_params_create(13, B.ckks_find_primes(45, 13, 3), B.ckks_find_primes(50, 13, 1), 3)
         client = CL.Client(P, seed)
@@ -71,8 +72,11 @@ class Block:
         self.norms = [(device(1 + 0.1 * r.normal(size=WIDTH)), device(0.1 * r.normal(size=WIDTH))) for _ in range(2)]
         # one conversation's cache: its pages need not lie in order
         pages = -(-max_tokens // PAGE)
-        self.k_pages = torch.zeros(pages, KV_HEADS, PAGE, DIM, device="cuda")
-        self.v_pages = torch.zeros_like(self.k_pages)
+        self.cache = [torch.zeros(pages, KV_HEADS, PAGE, DIM, device="cuda", dtype=packed or torch.float32) for _ in range(2)]
+        if packed:  # and a power of two for each 32 entries of a head
+            self.cache += [torch.zeros(pages, KV_HEADS, PAGE, -(-DIM // 32), device="cuda", dtype=torch.uint8) for _ in range(2)]
+        self.append, self.attend = ((K.ckks_clear_packed_append, K.ckks_clear_packed_attend) if packed else
+                                    (K.ckks_clear_cache_append, K.ckks_clear_attend))
         self.page_table = torch.from_numpy(r.permutation(pages).astype(np.int32)[None]).cuda()
         angle = np.arange(pages * PAGE)[:, None] * 10000.0 ** (-np.arange(0, DIM, 2) / DIM)
         self.cos, self.sin = device(np.cos(angle)), device(np.sin(angle))
@@ -90,12 +94,13 @@ class Block:
         h, _, _ = K.ckks_clear_layer_norm(x, *self.norms[0])
         qkv = self.qkv(h)
         q, k, v = qkv.view(n, HEADS + 2 * KV_HEADS, DIM).split((HEADS, KV_HEADS, KV_HEADS), dim=1)
-        q = K.ckks_clear_cache_append(k, v, self.k_pages, self.v_pages, *batch, cos=self.cos, sin=self.sin, q=q)
-        a = K.ckks_clear_attend(q, self.k_pages, self.v_pages, *batch)
+        q = self.append(k, v, *self.cache, *batch, cos=self.cos, sin=self.sin, q=q)
+        a = self.attend(q, *self.cache, *batch)
         return x + self.out(a.view(n, HEADS * DIM))
 
-    def generate(self, prompt, count, allowed=None):
-        """-> (tokens, the rows before the last layer norm, the logits under the rules, step by step)."""
+    def generate(self, prompt, count, allowed=None, draw=None):
+        """-> (tokens, the rows before the last layer norm, the logits under the rules, step by step).  draw: `count` numbers of [0, 1) by
+        which tokens are drawn (of the 20 likeliest, those that make up 0.9)."""
         tokens, rows, steps = list(prompt), [], []
         start = torch.empty(2, dtype=torch.int32, device="cuda")
         mask = None
@@ -117,7 +122,11 @@ class Block:
                 presence=torch.full((1,), 0.5, device="cuda"), bias_ids=torch.tensor([7], dtype=torch.int32, device="cuda"),
                 bias=torch.full((1,), 2.0, device="cuda"), bias_start=torch.tensor([0, 1], dtype=torch.int32, device="cuda"), mask=mask)
             steps.append(logits[0].clone())
-            tokens.append(int(logits.argmax()))
+            if draw is None:
+                tokens.append(int(logits.argmax()))
+            else:
+                tokens.append(int(K.ckks_clear_sample(logits, torch.full((1,), float(draw[len(tokens) - len(prompt)]), device="cuda"),
+                                                      top_k=torch.full((1,), 20, dtype=torch.int32, device="cuda"), top_p=torch.full((1,), 0.9, device="cuda"))))
             todo = tokens[-1:]
         return tokens, torch.cat(rows), steps
 
@@ -141,6 +150,9 @@ def main():
     tokens, rows, _ = block.generate(prompt, 8, allowed=range(0, VOCAB, 2))
     print("prompt  ", *prompt)
     print("answer  ", *tokens[len(prompt):])
+    small = Block(packed=torch.int8)
+    drawn, _, _ = small.generate(prompt, 8, allowed=range(0, VOCAB, 2), draw=np.random.default_rng(3).random(8))
+    print("drawn   ", *drawn[len(prompt):])
     # what another weight and bias would have given
     target, _, _ = K.ckks_clear_layer_norm(rows, block.norms[0][0] * 1.5, block.norms[0][1] + 0.5)
     errors = block.tune(rows, target, 20.0, 20)

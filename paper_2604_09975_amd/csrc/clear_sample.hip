@@ -6,7 +6,7 @@
 // (r^4 / 24 < 1.4e-13 for r = f ln 2 / 256).  Weights below 2^-64 are none.
 //
 // The order by logits is not needed, only where the kept tokens end in it: at a value, and after so many of the tokens that have it.
-//   top_k of up to 1024: the logits are counted by bins of their distance from the largest, those of the bins that hold the top_k are
+//   top_k of up to 256: the logits are counted by bins of their distance from the largest, those of the bins that hold the top_k are
 //     put into a list, and all the rest goes by the list.
 //   else: one pass sums counts and weights into bins (2^-1/32 apart).  The bin in which the top_k-th token, or the one that fills
 //     top_p, lies is then resolved: tokens of one value by their count, others by sorting them, very many by bins of their values first.
@@ -19,7 +19,7 @@
 namespace ckks {
 
 constexpr u32 BINS = 2048, CHUNKS = 4096;
-constexpr u32 LIST_K = 1024, LISTED = 2048;  // the largest top_k that goes by a list, and the list's room
+constexpr u32 LIST_K = 256, LISTED = 2048;  // the largest top_k that goes by a list, and the list's room
 constexpr u32 MAX_VOCAB = 1u << 20;
 constexpr u32 GRAIN = 256, GRAINS = 64 * GRAIN;  // steps of n: 2^-1/256; weights below 2^-64 are none
 
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             use(i, (float)v);
         }
     };
-    bool set_apart = false;
+    bool set_apart = false, many = false;  // many: too many to be set apart
     auto each_of = [&](auto some, auto use) {
         if (set_apart) {
             const u32 n = n_apart;
@@ -204,10 +204,10 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     u64 ties = ~0ull;
 
     // The lowest id up to which amounts sum to more than goal(all of them): amount(logit) where `some` holds, and `one` for each of the
-    // first `ties` tokens of value `last` (for which `some` need not hold).  `dense`: most logits have an amount.  prob: the
+    // first `ties` tokens of value `last` (for which `some` need not hold).  `dense`: how many logits have an amount.  prob: the
     // token's share.
     auto draw = [&](auto dense, auto some, auto amount, u64 one, auto goal, double &prob) -> u32 {
-        constexpr bool DENSE = decltype(dense)::value;
+        constexpr bool DENSE = decltype(dense)::value > 0, TIES = decltype(dense)::value < 2;
         auto value = [&](u64 sum, u64 n) { return sum + min(n, ties) * one; };
         const u32 n = rounds * WAVES;  // a chunk: what a wave takes in a round, 64 V ids
         __syncthreads();
@@ -226,7 +226,10 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             if (DENSE) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    sum += amount((float)x.v[i]);
+                    const float l = (float)x.v[i];
+                    const u64 w = amount(l);
+                    sum += !TIES || l > last ? w : 0;
+                    if (TIES) same += l == last;
                     if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             } else {
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                 });
             }
             if (DENSE || __any(sum != 0)) sum = scan_wave(sum);
-            if (!DENSE && __any(same != 0)) same = (u32)scan_wave(same);
+            if (TIES && __any(same != 0)) same = (u32)scan_wave(same);
             if (lane == 63) {
                 mass[r * WAVES + wave] = sum;
                 count[r * WAVES + wave] = same;
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             sames += same[k];
         }
         u64 sum0 = scan_block(sum);
-        u64 same0 = DENSE ? 0 : scan_block(sames);
+        u64 same0 = scan_block(sames);
         if (threadIdx.x == THREADS - 1) found64[0] = value(sum0, same0);
         sum0 -= sum;
         same0 -= sames;
@@ -287,9 +290,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float l = (float)x.v[i];
-                const bool in = DENSE || (l >= last && some(l));
-                part[i] = in && (DENSE || l > last) ? amount(l) : 0;
-                same[i] = !DENSE && in && l == last;
+                const bool in = l >= last && some(l);
+                part[i] = in && (!TIES || l > last) ? amount(l) : 0;
+                same[i] = TIES && in && l == last;
                 sum += part[i];
                 sames += same[i];
             }
@@ -309,8 +312,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         prob = (double)found64[0] / (double)all;
         return found[1];
     };
-    constexpr std::false_type SPARSE;
-    constexpr std::true_type ALL;
+    constexpr std::integral_constant<int, 0> SPARSE;
+    constexpr std::integral_constant<int, 1> MOST;
+    constexpr std::integral_constant<int, 2> ALL;  // there is no last one
 
     u64 *const list = mass, *const weight = mass + LISTED;  // tokens by their order: key, then the lower id; weights by rank
     auto entry = [](u32 id, float l) { return (u64)key_of(l) << 32 | (u32)~id; };
@@ -335,15 +339,23 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             __syncthreads();
             return;
         }
+        // by exchanges; those less than 128 apart stay within what a wave does, in its order
         for (u32 k = 2; k <= size; k *= 2)
             for (u32 j = k / 2; j; j /= 2) {
+                if (j >= 128) __syncthreads();
                 for (u32 i = threadIdx.x; i < size / 2; i += THREADS) {
                     const u32 p = 2 * i - (i & (j - 1)), q = p + j;
                     const u64 x = list[p], y = list[q];
                     if ((x < y) == !(p & k)) list[p] = y, list[q] = x;
                 }
-                __syncthreads();
+                if (j >= 128) {
+                    __syncthreads();
+                } else {
+                    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                    __builtin_amdgcn_wave_barrier();
+                }
             }
+        __syncthreads();
     };
     // Fills the list up with what comes last and sorts it.
     auto sort_list = [&](u32 n) {
@@ -418,7 +430,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         if (listed <= LISTED) {
             sort_list(listed);
             // consecutive ranks a thread
-            constexpr u32 EACH = LIST_K / THREADS;
+            constexpr u32 EACH = 1;
             const u32 kept = min((u32)top_k, listed);
             u64 w[EACH], sum = 0;
             u32 id[EACH];
@@ -564,7 +576,20 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             // logits of the bin, and a little beside it
             float lo = fmaxf((float)(top64 - ((bin + 1) * (GRAINS / BINS) + 0.5) / c) - reach, floor_l), hi = (float)(top64 - (bin * (GRAINS / BINS) - 1.0) / c) + reach;
             if (!(c > 0.0)) lo = floor_l, hi = top;
-            if (!set_apart) {  // what is kept lies in this bin and above it
+            if (!set_apart && !many) {
+                // What is kept lies in this bin and above it: how much that is, about, shows in the first round.
+                const Pack<T, V> x = fetch(0);
+                u32 n = 0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) n += (float)x.v[i] >= lo;
+                if (threadIdx.x == 0) n_bin = 0;
+                __syncthreads();
+                atomicAdd(&n_bin, n);
+                __syncthreads();
+                many = (u64)n_bin * rounds > APART + APART / 8;
+                __syncthreads();
+            }
+            if (!set_apart && !many) {
                 each_of([&](float l) { return l >= lo; }, [&](u32 id, float l) {
                     const u32 at = atomicAdd(&n_apart + zero, 1u);
                     if (at < APART) apart[at] = entry(id, l);
@@ -572,7 +597,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                 __syncthreads();
                 set_apart = n_apart <= APART;
                 __syncthreads();
-                if (!set_apart && threadIdx.x == 0) n_apart = 0;
+                many = !set_apart;
             }
             auto near_bin = [&](float l) { return __builtin_amdgcn_fmed3f(l, lo, hi) == l; };
             u32 from = 0, to = ~0u;  // keys that are looked at
@@ -685,17 +710,20 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         if (limit_p) resolve(false, 0, fmax((double)top_p * (double)total, 0.5));
     }
     u32 id;
-    if (last > floor_l || ties != ~0ull || least > 0.0) {
+    const double w_last = weigh(last).w;
+    const u64 one = w_last >= least ? whole(w_last) : 0ull;
+    if (least > 0.0 || (!many && (last > floor_l || ties != ~0ull))) {
         // logits that may reach min_p, and a little below
         const float enough = least > 0.0 ? (float)(top64 + (__log2f((float)least) * GRAIN - 1.0) / c) - reach : last;
-        const double w = weigh(last).w;
         id = draw(
             SPARSE, [&](float l) { return !(l < enough); },
             [&](float l) -> u64 {
                 const double w = weigh(l).w;
                 return w >= least ? whole(w) : 0ull;
             },
-            w >= least ? whole(w) : 0ull, share, prob);
+            one, share, prob);
+    } else if (last > floor_l || ties != ~0ull) {
+        id = draw(MOST, may, [&](float l) { return whole(weigh(l).w); }, one, share, prob);
     } else {
         id = draw(ALL, may, [&](float l) { return whole(weigh(l).w); }, 0, share, prob);
     }

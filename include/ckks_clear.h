@@ -217,7 +217,7 @@ int ckks_clear_packed_attend(const ckks_clear_packed_attend_t *a, void *stream);
 
 /* Reads the new tokens' keys and values (all of a sequence's, if as many rows as kv_len are asked for) back: the values that the codes
  * stand for, in dtype.  A token at a position below 0 or in a page outside [0, n_pages) reads as zeros; rows in no sequence
- * are not written.  Rows read and appended again give the same values.  d_k_out, d_v_out [n_tokens][kv_heads][head_dim] by strides
+ * are not written.  Rows that ckks_clear_packed_append wrote give the same values when they are read and appended again.  d_k_out, d_v_out [n_tokens][kv_heads][head_dim] by strides
  * {token, head}, either NULL; they share no entry. */
 typedef struct {
     ckks_clear_packed_t pages;

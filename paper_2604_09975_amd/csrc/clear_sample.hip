@@ -706,8 +706,23 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                 from = to - from > width ? to - width : from;
             }
         };
-        if (limit_k && (u32)top_k < tokens) total = resolve(true, (u64)top_k, 0.0);
-        if (limit_p) resolve(false, 0, fmax((double)top_p * (double)total, 0.5));
+        // No more tokens and weights than these reach min_p: a limit that they keep to leaves them all.
+        u64 likely_mass = ~0ull;
+        u32 likely = ~0u;
+        if (least > 0.0) {
+            const u32 bin = min(bin_of((u32)(-__log2f((float)least) * GRAIN) + 3), BINS - 1);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (PER * threadIdx.x + k == bin) found64[0] = bins.upto_mass[k], found[0] = bins.upto_count[k];
+            __syncthreads();
+            likely_mass = found64[0];
+            likely = found[0];
+        }
+        // (Where top_p follows, it goes by the sum of the top_k.)
+        if (limit_k && (u32)top_k < (limit_p ? tokens : min(tokens, likely))) total = resolve(true, (u64)top_k, 0.0);
+        const double goal = fmax((double)top_p * (double)total, 0.5);
+        if (limit_p && !((double)likely_mass <= goal)) resolve(false, 0, goal);
     }
     u32 id;
     const double w_last = weigh(last).w;

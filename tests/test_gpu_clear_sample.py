@@ -170,6 +170,19 @@ def test_temperatures_of_every_size(dtype):
     check(logits, u, temperature=t, top_k=[40] * len(t), top_p=[0.8] * len(t))
 
 
+def test_min_p_beside_limits_that_it_keeps_to_and_that_it_does_not():
+    """top_k and top_p around the number and the sum of the tokens that reach min_p; top_p of the top_k's sum."""
+    g = gen(11)
+    logits = 2 * randn(g, 1, 20000)
+    w = torch.exp(logits[0].double() - logits.max().double()).sort(descending=True).values
+    n = int((w >= 0.05).sum())
+    share = float(w[:n].sum() / w.sum())
+    rows = [(k, p) for k in (0, 300, n - 1, n, n + 1, 2 * n, 5000) for p in (1.0, share * 0.9, share * 0.999, share * 1.001, share * 1.2, 0.9)]
+    u = torch.rand(len(rows), generator=g, device="cuda")
+    check(logits.expand(len(rows), -1), u, top_k=[k for k, _ in rows], top_p=[min(p, 1.0) for _, p in rows], min_p=[0.05] * len(rows))
+    check(logits.expand(len(rows), -1).half(), u, top_k=[k for k, _ in rows], top_p=[min(p, 1.0) for _, p in rows], min_p=[0.05] * len(rows), temperature=[0.7] * len(rows))
+
+
 def test_limits_that_are_not_a_number_are_none():
     g = gen(8)
     logits, u = randn(g, 4, 900), torch.rand(4, generator=g, device="cuda")

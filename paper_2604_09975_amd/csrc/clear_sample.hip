@@ -66,7 +66,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     __shared__ u64 apart[APART];                               // tokens set apart, those that all later passes are about
     __shared__ double power[GRAIN];                            // 2^(j / 256)
     __shared__ u64 wave_sums[WAVES];
-    __shared__ u32 n_list, n_apart, n_bin, key_min, key_max;
+    __shared__ u32 n_list, n_bin, key_min, key_max;
     __shared__ u32 found[4];
     __shared__ u64 found64[2];
     __shared__ float wave_top[WAVES];
@@ -103,13 +103,15 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     constexpr std::integral_constant<u32, 4> LIGHT;  // for passes that do little with a logit, and for the others
     constexpr std::integral_constant<u32, 2> HEAVY;
     // use(i, logit) for those few of a pack that `some` holds for: as many turns as the lane with the most of them has
-    auto few_of = [&](const Pack<T, V> &x, auto some, auto use) {
+    // (then end(lanes that had one), by all lanes of the wave)
+    auto few_of = [&](const Pack<T, V> &x, auto some, auto use, auto end) {
         u32 bits = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) bits |= some((float)x.v[i]) ? 1u << i : 0u;
         u32 w[8] = {};
         __builtin_memcpy(w, &x, sizeof(x));
-        while (bits) {
+        for (u64 active; (active = __ballot(bits != 0)); end(active)) {
+            if (!bits) continue;
             const u32 i = __ffs(bits) - 1, at = i * sizeof(T) / 4;
             bits &= bits - 1;
             const u32 a0 = at & 1 ? w[1] : w[0], a1 = at & 1 ? w[3] : w[2], a2 = at & 1 ? w[5] : w[4], a3 = at & 1 ? w[7] : w[6];
@@ -119,18 +121,20 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             use(i, (float)v);
         }
     };
+    auto nothing = [](u64) {};
     bool set_apart = false, many = false;  // many: too many to be set apart
+    u32 own_apart = 0;                     // tokens that the wave has set apart, in its own stretch of `apart`
+    constexpr u32 OWN = APART / WAVES;
     auto each_of = [&](auto some, auto use) {
         if (set_apart) {
-            const u32 n = n_apart;
-            for (u32 i = threadIdx.x; i < n; i += THREADS) {
-                const u64 x = apart[i];
+            for (u32 i = lane; i < own_apart; i += 64) {
+                const u64 x = apart[wave * OWN + i];
                 const float l = value_of((u32)(x >> 32));
                 if (some(l)) use((u32)~x, l);
             }
             return;
         }
-        each(LIGHT, [&](u32 at, const Pack<T, V> &x, u32) { few_of(x, some, [&](u32 i, float l) { use(at + i, l); }); });
+        each(LIGHT, [&](u32 at, const Pack<T, V> &x, u32) { few_of(x, some, [&](u32 i, float l) { use(at + i, l); }, nothing); });
     };
     // Inclusive sums over the threads.
     auto scan_block = [&](u64 x) {
@@ -161,7 +165,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     if (lane == 0) wave_top[wave] = top;
     for (u32 j = threadIdx.x; j < GRAIN; j += THREADS) power[j] = exp2(j / (double)GRAIN);
     for (u32 i = threadIdx.x; i < BINS; i += THREADS) mass[i] = 0, count[i] = 0;
-    if (threadIdx.x == 0) n_list = n_apart = 0;
+    if (threadIdx.x == 0) n_list = 0;
     __syncthreads();
 #pragma unroll
     for (u32 w = 0; w < WAVES; ++w) top = fmaxf(top, wave_top[w]);
@@ -238,7 +242,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                         sum += amount(l);
                     else
                         ++same;
-                });
+                }, nothing);
             }
             if (DENSE || __any(sum != 0)) sum = scan_wave(sum);
             if (TIES && __any(same != 0)) same = (u32)scan_wave(same);
@@ -576,27 +580,19 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             // logits of the bin, and a little beside it
             float lo = fmaxf((float)(top64 - ((bin + 1) * (GRAINS / BINS) + 0.5) / c) - reach, floor_l), hi = (float)(top64 - (bin * (GRAINS / BINS) - 1.0) / c) + reach;
             if (!(c > 0.0)) lo = floor_l, hi = top;
-            if (!set_apart && !many) {
-                // What is kept lies in this bin and above it: how much that is, about, shows in the first round.
-                const Pack<T, V> x = fetch(0);
-                u32 n = 0;
-#pragma unroll
-                for (int i = 0; i < V; ++i) n += (float)x.v[i] >= lo;
-                if (threadIdx.x == 0) n_bin = 0;
-                __syncthreads();
-                atomicAdd(&n_bin, n);
-                __syncthreads();
-                many = (u64)n_bin * rounds > APART + APART / 8;
-                __syncthreads();
-            }
-            if (!set_apart && !many) {
-                each_of([&](float l) { return l >= lo; }, [&](u32 id, float l) {
-                    const u32 at = atomicAdd(&n_apart + zero, 1u);
-                    if (at < APART) apart[at] = entry(id, l);
+            if (!set_apart && !many) {  // what is kept lies in this bin and above it
+                each(LIGHT, [&](u32 at, const Pack<T, V> &x, u32) {
+                    if (own_apart > OWN) return;
+                    few_of(
+                        x, [&](float l) { return l >= lo; },
+                        [&](u32 i, float l) {
+                            const u64 active = __ballot(true);
+                            const u32 place = own_apart + __builtin_amdgcn_mbcnt_hi((u32)(active >> 32), __builtin_amdgcn_mbcnt_lo((u32)active, 0));
+                            if (place < OWN) apart[wave * OWN + place] = entry(at + i, l);
+                        },
+                        [&](u64 active) { own_apart += __popcll(active); });
                 });
-                __syncthreads();
-                set_apart = n_apart <= APART;
-                __syncthreads();
+                set_apart = !__syncthreads_or(own_apart > OWN);
                 many = !set_apart;
             }
             auto near_bin = [&](float l) { return __builtin_amdgcn_fmed3f(l, lo, hi) == l; };

@@ -41,8 +41,14 @@ __device__ __forceinline__ void unpack4(u32 codes, float power, T *out) {
             out[0] = lo[0], out[1] = lo[1], out[2] = hi[0], out[3] = hi[1];
         }
     } else {
+        // (as a vector: number by number the compiler converts each alone and joins pairs by shifts; prompts of I8 1776 -> 1655 us)
+        typedef float f32s __attribute__((ext_vector_type(4)));
+        typedef T cells __attribute__((ext_vector_type(4)));
+        f32s x;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = (T)((float)(signed char)(codes >> 8 * i) * power);
+        for (int i = 0; i < 4; ++i) x[i] = (float)(signed char)(codes >> 8 * i);
+        const cells y = __builtin_convertvector(x * power, cells);
+        __builtin_memcpy(out, &y, sizeof(y));
     }
 }
 // 16 bytes of T out of a piece of their codes.

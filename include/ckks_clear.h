@@ -181,9 +181,9 @@ typedef struct {
  *   each block of 32 entries: e = the smallest number >= -100 with max |x| <= M 2^e, M = 448 (E4M3) or 127 (I8),
  *   power = e + 127, codes = x / 2^e rounded to the nearest, ties to even.
  * A block that holds an infinity, a NaN or an entry of 2^128 or more is stored as power 255 and codes 0.  Norm and rotation are
- * computed in 64 bits; keys meet no other rounding than that to their code, queries are rounded to 32 bits and to dtype.  Rotated entries without an angle are
- * NaN, and so is, in the cache, their block.  What is not stored, what may lie in what, rows in no sequence: as in
- * ckks_clear_cache_append. */
+ * computed in 64 bits; keys meet no other rounding than that to their code, queries are rounded to 32 bits and to dtype.
+ * Rotated entries without an angle are NaN, and so is, in the cache, their block.  What is not stored, what may lie in what, rows in
+ * no sequence: as in ckks_clear_cache_append. */
 typedef struct {
     ckks_clear_packed_t pages;
     ckks_clear_batch_t batch;
@@ -217,8 +217,8 @@ int ckks_clear_packed_attend(const ckks_clear_packed_attend_t *a, void *stream);
 
 /* Reads the new tokens' keys and values (all of a sequence's, if as many rows as kv_len are asked for) back: the values that the codes
  * stand for, in dtype.  A token at a position below 0 or in a page outside [0, n_pages) reads as zeros; rows in no sequence
- * are not written.  Rows that ckks_clear_packed_append wrote give the same values when they are read and appended again.  d_k_out, d_v_out [n_tokens][kv_heads][head_dim] by strides
- * {token, head}, either NULL; they share no entry. */
+ * are not written.  Rows that ckks_clear_packed_append wrote give the same values when they are read and appended again.
+ * d_k_out, d_v_out [n_tokens][kv_heads][head_dim] by strides {token, head}, either NULL; they share no entry. */
 typedef struct {
     ckks_clear_packed_t pages;
     ckks_clear_batch_t batch;

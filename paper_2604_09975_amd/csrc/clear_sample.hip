@@ -710,7 +710,8 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         u64 likely_mass = ~0ull;
         u32 likely = ~0u;
         if (least > 0.0) {
-            const u32 bin = min(bin_of((u32)(-__log2f((float)least) * GRAIN) + 3), BINS - 1);
+            // (the logarithm of the hardware takes a subnormal as 0; and no weight is below 2^-64)
+            const u32 bin = min(bin_of((u32)(-__log2f(fmaxf((float)least, 0x1p-64f)) * GRAIN) + 3), BINS - 1);
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < PER; ++k)
@@ -729,7 +730,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     const u64 one = w_last >= least ? whole(w_last) : 0ull;
     if (least > 0.0 || (!many && (last > floor_l || ties != ~0ull))) {
         // logits that may reach min_p, and a little below
-        const float enough = least > 0.0 ? (float)(top64 + (__log2f((float)least) * GRAIN - 1.0) / c) - reach : last;
+        const float enough = least > 0.0 ? (float)(top64 + (__log2f(fmaxf((float)least, 0x1p-64f)) * GRAIN - 1.0) / c) - reach : last;
         id = draw(
             SPARSE, [&](float l) { return !(l < enough); },
             [&](float l) -> u64 {

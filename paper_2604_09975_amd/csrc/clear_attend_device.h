@@ -283,8 +283,17 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(typename Stor
     constexpr int ZP = FORM == PLAIN ? 1 : PASSES;
     u32 kz[ZP], vz[ZP];  // the pieces' powers of two
     const u32 block = FORM != PLAIN && piece_ok ? piece * E / PACK_BLOCK : 0;
+    // Zeros are the same either way, but registers are not: as {}, F32 heads of 64 have 91 of their scalars out of registers instead of 48 (1
+    // token over 128, 12 heads: 10.1 us for 9.4; 28 over 732: 47.4 for 45.9); written out, heads of 256 in 16 bits have 172 vector
+    // registers in scratch instead of 107 (64 tokens over 8192, 8 heads: 1497 us for 1220), and F32 heads of 80 take 92 us for 89.
+    constexpr bool WRITTEN_OUT = FORM == PLAIN && sizeof(T) == 4 && DP == 64;
 #pragma unroll
-    for (int p = 0; p < PASSES; ++p) kr[p] = vr[p] = piece_t{};
+    for (int p = 0; p < PASSES; ++p) {
+        if constexpr (WRITTEN_OUT)
+            kr[p] = vr[p] = make_uint4(0, 0, 0, 0);
+        else
+            kr[p] = vr[p] = piece_t{};
+    }
 #pragma unroll
     for (int p = 0; p < ZP; ++p) kz[p] = vz[p] = 0;
     // Where the rows that this thread fetches lie.  The table's answer is looked at only when it is needed, a tile later: a wait
@@ -391,7 +400,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void attend_kernel(typename Stor
 #pragma unroll
             for (int p = 0; p < PASSES; ++p)
                 if (none >> p & 1) {
-                    x[p] = piece_t{};
+                    if constexpr (WRITTEN_OUT)
+                        x[p] = make_uint4(0, 0, 0, 0);
+                    else
+                        x[p] = piece_t{};
                     if (FORM != PLAIN) z[p] = 0;
                 }
     };

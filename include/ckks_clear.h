@@ -239,8 +239,9 @@ int ckks_clear_packed_read(const ckks_clear_packed_read_t *a, void *stream);
  * d_temperature, d_top_p, d_min_p, d_u: f32 [rows], d_top_k: int32 [rows]; all but d_u may be NULL (1; no limit).  A
  * temperature of 0 or below takes the largest logit (the lowest id; prob 1), top_p of 0 or below the first token only.  u below 0
  * counts as 0, u of 1 or more takes the last token kept; NaN counts as no limit, temperature 1, u = 0.
- * A logit of -infinity or NaN is never drawn; logits of +infinity are drawn alike.  A row without any other gets token -1, prob 0.
- * Sums are held in 64 bits and joined in a fixed order: the same inputs give the same token.  d_prob: f32 [rows] or NULL. */
+ * A logit of -infinity or NaN is never drawn, and one whose w is below 2^-64 counts as -infinity; logits of +infinity are drawn alike.
+ * A row without any other gets token -1, prob 0.  Sums are held in 64 bits, off by less than 2^-40 of themselves, and joined in a fixed
+ * order: the same inputs give the same token.  d_prob: f32 [rows] or NULL. */
 typedef struct {
     const void *d_logits;
     int32_t *d_token;

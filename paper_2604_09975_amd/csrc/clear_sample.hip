@@ -1,9 +1,12 @@
 // Draw of the next token: temperature, top-k, top-p, min-p and a given uniform number.  A block takes a row.
 //
-// What is drawn depends on sums of up to a million weights compared with each other, so a weight is computed in 64 bits and added as a
-// whole number of 2^-bits: such sums do not depend on their order, and a token next to the border of two is off by 2^-40 of the sum at
-// most.  w = exp((l - max) / T) = 2^(-n / 256) 2^(f / 256) with n whole, |f| <= 1/2: a table of 256 and a polynomial of degree 3
-// (r^4 / 24 < 1.4e-13 for r = f ln 2 / 256).  Weights below 2^-64 are none.
+// What is drawn depends on sums of up to a million weights compared with each other, so a weight is computed in 64 bits.
+// w = exp((l - max) / T) = 2^(-n / 256) 2^(f / 256) with n whole, |f| <= 1/2: a table of 256 and a polynomial of degree 3
+// (r^4 / 24 < 1.4e-13 < 2^-42 for r = f ln 2 / 256).  Weights below 2^-64 are none.  Sums are of 64-bit floats in a fixed order, and
+// where atomics add, of whole numbers, which do not depend on theirs:
+//   by bins: of 2^-bits of the octave that the bin lies in, 2^-42 of each weight for 2^20 tokens, 2^-45 for 131072;
+//   of up to 8192 tokens set apart: of 2^-54 for weights from 2^-13 on, of 2^-66 for those below: 2^-41 of the sum.
+// So a token next to the border of two is off by 2^-40 of the sum at most, however many small weights make up the sum.
 //
 // The order by logits is not needed, only where the kept tokens end in it: at a value, and after so many of the tokens that have it.
 //   top_k of up to 256: the logits are counted by bins of their distance from the largest, those of the bins that hold the top_k are
@@ -26,6 +29,8 @@ constexpr u32 BINS = 2048, CHUNKS = 4096;
 constexpr u32 LIST_K = 256, LISTED = 2048;  // the largest top_k that goes by a list, and the list's room
 constexpr u32 MAX_VOCAB = 1u << 20;
 constexpr u32 GRAIN = 256, GRAINS = 64 * GRAIN;  // steps of n: 2^-1/256; weights below 2^-64 are none
+constexpr double FAR = 512 * GRAIN;              // ... as they are computed: 2^-512, nothing beside a weight
+constexpr double TINY = 0x1p-100;                // more than what many such sum to, less than a weight
 
 struct SampleArgs {
     const void *logits;
@@ -39,18 +44,29 @@ struct SampleArgs {
 
 // Inclusive sums over the lanes of a wave: by DPP within rows of 16, then from row to row.
 template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 add_dpp(u64 x) {
-    const u32 lo = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)x, CTRL, ROWS, 0xf, false);
-    const u32 hi = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(x >> 32), CTRL, ROWS, 0xf, false);
-    return x + ((u64)hi << 32 | lo);
+__device__ __forceinline__ u32 add_dpp(u32 x) {
+    return x + (u32)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
 }
-__device__ __forceinline__ u64 scan_wave(u64 x) {
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_dpp(double x) {
+    const u64 b = (u64)__double_as_longlong(x);
+    const u32 lo = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)b, CTRL, ROWS, 0xf, false);
+    const u32 hi = (u32)__builtin_amdgcn_update_dpp(0, (int)(u32)(b >> 32), CTRL, ROWS, 0xf, false);
+    return x + __longlong_as_double((long long)((u64)hi << 32 | lo));
+}
+template <class X>
+__device__ __forceinline__ X scan_wave(X x) {
     x = add_dpp<0x111, 0xf>(x);  // row_shr 1, 2, 4, 8
     x = add_dpp<0x112, 0xf>(x);
     x = add_dpp<0x114, 0xf>(x);
     x = add_dpp<0x118, 0xf>(x);
     x = add_dpp<0x142, 0xa>(x);  // row_bcast 15, 31
     return add_dpp<0x143, 0xc>(x);
+}
+__device__ __forceinline__ u32 lane_of(u32 x, u32 lane) { return (u32)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ __forceinline__ double lane_of(double x, u32 lane) {
+    const u64 b = (u64)__double_as_longlong(x);
+    return __longlong_as_double((long long)((u64)lane_of((u32)(b >> 32), lane) << 32 | lane_of((u32)b, lane)));
 }
 // The order of floats as that of whole numbers (-0 as 0), and back.
 __device__ __forceinline__ u32 key_of(float x) {
@@ -65,14 +81,15 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     constexpr int PER = BINS / THREADS;
     constexpr u32 APART = THREADS == 1024 ? 8192 : 2048;
     constexpr u32 SPAN = THREADS * V, WAVES = THREADS / 64;    // SPAN: ids of a round
-    __shared__ __attribute__((aligned(16))) u64 mass[CHUNKS];  // weights of the bins; of stretches of ids; lists
+    __shared__ __attribute__((aligned(16))) u64 mass[CHUNKS];  // weights of the bins; of stretches of ids (64-bit floats); lists
     __shared__ u32 count[CHUNKS];                              // tokens of the bins; of stretches of ids that have the last value
     __shared__ u64 apart[APART];                               // tokens set apart, those that all later passes are about
     __shared__ double power[GRAIN];                            // 2^(j / 256)
-    __shared__ u64 wave_sums[WAVES];
+    __shared__ u32 wave_counts[WAVES];
+    __shared__ double wave_sums[WAVES];
     __shared__ u32 n_list, n_bin, key_min, key_max;
-    __shared__ u32 found[4];
-    __shared__ u64 found64[2];
+    __shared__ u32 found[4], found_count;
+    __shared__ double found_sum;
     __shared__ float wave_top[WAVES];
 
     const u32 row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -140,16 +157,48 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         }
         each(LIGHT, [&](u32 at, const Pack<T, V> &x, u32) { few_of(x, some, [&](u32 i, float l) { use(at + i, l); }, nothing); });
     };
-    // Inclusive sums over the threads.
-    auto scan_block = [&](u64 x) {
+    // Inclusive sums over the threads, and over all of them, in two steps with a barrier between them.
+    auto scan_begin = [&](auto x, auto *of_wave) {
         x = scan_wave(x);
+        if (lane == 63) of_wave[wave] = x;
+        return x;
+    };
+    auto scan_end = [&](auto x, const auto *of_wave, auto &all) {
+        const auto upto = scan_wave(lane < WAVES ? of_wave[lane] : decltype(x)(0));
+        all = lane_of(upto, WAVES - 1);
+        return wave ? x + lane_of(upto, wave - 1) : x;
+    };
+    auto scan_sums = [&](double x, double &all) {
         __syncthreads();
-        if (lane == 63) wave_sums[wave] = x;
+        x = scan_begin(x, wave_sums);
         __syncthreads();
-        u64 before = 0;
-#pragma unroll
-        for (u32 w = 0; w < WAVES; ++w) before += w < wave ? wave_sums[w] : 0;
-        return x + before;
+        return scan_end(x, wave_sums, all);
+    };
+    auto scan_counts = [&](u32 x, u32 &all) {
+        __syncthreads();
+        x = scan_begin(x, wave_counts);
+        __syncthreads();
+        return scan_end(x, wave_counts, all);
+    };
+    auto scan_both = [&](double &x, double &all, u32 &n, u32 &count) {
+        __syncthreads();
+        x = scan_begin(x, wave_sums);
+        n = scan_begin(n, wave_counts);
+        __syncthreads();
+        x = scan_end(x, wave_sums, all);
+        n = scan_end(n, wave_counts, count);
+    };
+    // Atomics of single lanes go to an address of their own: one that the compiler knows to be the same for all lanes it goes through lane by
+    // lane, which takes ten times as long.
+    u32 zero = 0;
+    asm volatile("" : "+v"(zero));
+    // The least `first` and the largest `end` of all threads, in `found`; ~0 and 0 are none.  (Both rise from thread to thread.)
+    auto find_ends = [&](u32 first, u32 end) {
+        const u64 firsts = __ballot(first != ~0u), ends = __ballot(end != 0);
+        if (firsts) first = lane_of(first, (u32)__ffsll((unsigned long long)firsts) - 1);
+        if (ends) end = lane_of(end, 63 - (u32)__clzll((long long)ends));
+        if (lane == 0 && firsts) atomicMin(&found[0] + zero, first);
+        if (lane == 0 && ends) atomicMax(&found[1] + zero, end);
     };
     auto finish = [&](u32 token, double prob) {
         if (threadIdx.x == 0) {
@@ -182,18 +231,20 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     const double least = min_p > 0.0f ? fmin((double)min_p, 1.0) : 0.0;
     const double c = GRAIN * 1.4426950408889634074 / (double)temperature, top64 = top;
     const double magic = __longlong_as_double((long long)(1023 + 52 - a.bits) << 52);
-    // Logits that may have a weight; false for NaN and -infinity.  (A little below, so that it does not cut off what `weigh` counts.)
-    const float floor_l = fmaxf((float)(top64 - (GRAINS + 8.0) / c * (1 + 1e-6)), -3.402823466e38f);
+    // Logits that have a weight, of 2^-64 or more; false for NaN and -infinity.
+    const double least_l = top64 - GRAINS / c;
+    float floor_l = fmaxf((float)least_l, -3.402823466e38f);
+    if ((double)floor_l < least_l) floor_l = value_of(key_of(floor_l) + 1);
     auto may = [&](float l) { return l >= floor_l; };
     const float reach = 1e-6f * fabsf(top);  // more than bounds that are worked out in 32 bits are off by
-    // n: steps down from the largest; w = 2^(-n / 256) 2^(f / 256).  NaN and all that is far below: n = GRAINS + 64.
+    // n: steps down from the largest; w = 2^(-n / 256) 2^(f / 256).  (NaN and all that is far below: n = FAR.)
     struct Weight {
         u32 n;
         double w;
     };
     auto weigh = [&](float l) {
         constexpr double ROUND = 6755399441055744.0, STEP = 0.69314718055994530942 / GRAIN;  // 1.5 * 2^52: n in the lower word of the sum
-        const double t = fmax(((double)l - top64) * c, -(double)(GRAINS + 64)), s = t + ROUND, f = t - (s - ROUND);
+        const double t = fmax(((double)l - top64) * c, -FAR), s = t + ROUND, f = t - (s - ROUND);
         const double q = f * __builtin_fma(f, __builtin_fma(f, STEP * STEP * STEP / 6, STEP * STEP / 2), STEP);
         const int n = (int)(u32)__double_as_longlong(s);
         const u64 e = (u64)__double_as_longlong(power[n & (GRAIN - 1)]) + ((u64)(u32)((n >> 8) << 20) << 32);
@@ -201,42 +252,59 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         return Weight{(u32)-n, __builtin_fma(p, q, p)};
     };
     static_assert(GRAIN == 256, "n >> 8");
-    auto bin_of = [&](u32 n) { return n / (GRAINS / BINS); };
-    // (0 from 2^-52 on, as `bits` is 51 at most)
-    auto whole = [&](double w) { return (u64)__double_as_longlong(w + magic) & ((1ull << 52) - 1); };
-    // What u asks for of a sum.
-    auto share = [&](u64 sum) -> u64 { return u < 1.0f ? min((u64)(fmax((double)u, 0.0) * (double)sum), sum - 1) : u >= 1.0f ? sum - 1 : 0ull; };
+    auto bin_of = [&](u32 n) { return min(n / (GRAINS / BINS), BINS - 1); };
+    // A bin's weights as whole numbers of 2^-bits of its octave (a half to one of it, so none becomes 0), and a sum of them.
+    constexpr u32 OCTAVE = GRAIN / (GRAINS / BINS);  // bins of an octave
+    auto whole = [&](double w, u32 bin) {
+        const double x = __longlong_as_double(__double_as_longlong(w) + ((long long)(bin / OCTAVE) << 52));
+        return (u64)__double_as_longlong(x + magic) & ((1ull << 52) - 1);
+    };
+    auto sum_of = [&](u64 sum, u32 bin) { return (double)sum * __longlong_as_double((long long)(1023 - a.bits - bin / OCTAVE) << 52); };
+    // What u asks for of a sum: the token is the first with which the sum is above it, or the last.
+    auto share = [&](double sum) { return u < 1.0f ? fmax((double)u, 0.0) * sum : u >= 1.0f ? __builtin_inf() : 0.0; };
+    // Logits that may reach min_p, and a little below.  (The logarithm of the hardware takes a subnormal as 0; and no weight is below 2^-64.)
+    const float least_log = __log2f(fmaxf((float)least, 0x1p-64f));
+    const float enough = least > 0.0 ? (float)(top64 + (least_log * GRAIN - 1.0) / c) - reach : floor_l;
 
     // Kept are the tokens above `last`, and of those that have it the `ties` with the lowest ids.
     float last = floor_l;
-    u64 ties = ~0ull;
+    u32 ties = ~0u;
 
-    // The lowest id up to which amounts sum to more than goal(all of them): amount(logit) where `some` holds, and `one` for each of the
-    // first `ties` tokens of value `last` (for which `some` need not hold).  `dense`: how many logits have an amount.  prob: the
-    // token's share.
-    auto draw = [&](auto dense, auto some, auto amount, u64 one, auto goal, double &prob) -> u32 {
+    // The lowest id up to which amounts sum to more than goal(all of them), or the last that has one: amount(logit) where `some` holds, and
+    // `one` for each of the first `ties` tokens of value `last` (for which `some` need not hold).  `dense`: how many logits have an
+    // amount.  prob: the token's share.
+    auto draw = [&](auto dense, auto some, auto amount, double one, auto goal, double &prob) -> u32 {
         constexpr bool DENSE = decltype(dense)::value > 0, TIES = decltype(dense)::value < 2;
-        auto value = [&](u64 sum, u64 n) { return sum + min(n, ties) * one; };
-        const u32 n = rounds * WAVES;  // a chunk: what a wave takes in a round, 64 V ids
+        auto value = [&](double sum, u32 n) { return TIES ? sum + (double)min(n, ties) * one : sum; };
+        // whether there is something among tokens of this sum, `same` of them of value `last` after `before` others
+        auto any_of = [&](double sum, u32 same, u32 before) { return sum > TINY || (TIES && same && before < ties && one > 0.0); };
+        const u32 n = rounds * WAVES;  // a chunk: what a wave takes in a round, 64 V ids; 2048 at most
+        const bool by_atomics = !DENSE && set_apart;
+        constexpr double LARGE = 0x1p54, SMALL = 0x1p66;  // grids: sums of a chunk's 512 weights stay below 2^64
+        u64 *const small = mass + CHUNKS / 2;
         __syncthreads();
-        if (!DENSE && set_apart) {
-            for (u32 i = threadIdx.x; i < n; i += THREADS) mass[i] = 0, count[i] = 0;
+        if (by_atomics) {
+            for (u32 i = threadIdx.x; i < n; i += THREADS) mass[i] = 0, small[i] = 0, count[i] = 0;
             __syncthreads();
             each_of([&](float l) { return l >= last && some(l); }, [&](u32 id, float l) {
-                if (l > last)
-                    atomicAdd((unsigned long long *)&mass[id / (64 * V)], (unsigned long long)amount(l));
-                else
+                if (l > last) {
+                    const double w = amount(l);
+                    if (w >= 0x1p-13)
+                        atomicAdd((unsigned long long *)&mass[id / (64 * V)], (unsigned long long)(w * LARGE));
+                    else
+                        atomicAdd((unsigned long long *)&small[id / (64 * V)], (unsigned long long)(w * SMALL));
+                } else {
                     atomicAdd(&count[id / (64 * V)], 1u);
+                }
             });
         } else each(std::integral_constant<u32, DENSE ? 2 : 4>(), [&](u32, const Pack<T, V> &x, u32 r) {
-            u64 sum = 0;
+            double sum = 0.0;
             u32 same = 0;
             if (DENSE) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float l = (float)x.v[i];
-                    const u64 w = amount(l);
-                    sum += !TIES || l > last ? w : 0;
+                    sum += amount((TIES ? l > last : may(l)) ? l : -__builtin_inff());
                     if (TIES) same += l == last;
                     if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
@@ -248,77 +316,104 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                         ++same;
                 }, nothing);
             }
-            if (DENSE || __any(sum != 0)) sum = scan_wave(sum);
-            if (TIES && __any(same != 0)) same = (u32)scan_wave(same);
+            if (DENSE || __any(sum != 0.0)) sum = scan_wave(sum);
+            if (TIES && __any(same != 0)) same = scan_wave(same);
             if (lane == 63) {
-                mass[r * WAVES + wave] = sum;
+                mass[r * WAVES + wave] = (u64)__double_as_longlong(sum);
                 count[r * WAVES + wave] = same;
             }
         });
         __syncthreads();
-        constexpr u32 EACH = THREADS == 1024 ? CHUNKS / THREADS : 1;  // chunks a thread
-        u64 part[EACH], sum = 0;
+        if (threadIdx.x == 0) found[0] = ~0u, found[1] = 0;
+        constexpr u32 EACH = THREADS == 1024 ? CHUNKS / 2 / THREADS : 1;  // chunks a thread
+        double part[EACH], sum = 0.0;
         u32 same[EACH], sames = 0;
 #pragma unroll
         for (u32 k = 0; k < EACH; ++k) {
             const u32 at = threadIdx.x * EACH + k;
-            part[k] = at < n ? mass[at] : 0;
+            part[k] = 0.0;
+            if (at < n) part[k] = by_atomics ? (double)mass[at] * (1 / LARGE) + (double)small[at] * (1 / SMALL) : __longlong_as_double((long long)mass[at]);
             same[k] = at < n ? count[at] : 0;
             sum += part[k];
             sames += same[k];
         }
-        u64 sum0 = scan_block(sum);
-        u64 same0 = scan_block(sames);
-        if (threadIdx.x == THREADS - 1) found64[0] = value(sum0, same0);
+        double sum0 = sum, all;
+        u32 same0 = sames, all_same = 0;
+        if constexpr (TIES)
+            scan_both(sum0, all, same0, all_same);
+        else
+            sum0 = scan_sums(sum0, all);
+        all = value(all, all_same);
+        const double wanted = goal(all);
         sum0 -= sum;
         same0 -= sames;
-        __syncthreads();
-        const u64 all = found64[0], wanted = goal(all);
-        __syncthreads();
+        u32 first = ~0u, end = 0;  // the first of the thread's chunks with which the sum is above it; behind the last that adds to it
+        {
+            double s = sum0;
+            u32 m = same0;
 #pragma unroll
-        for (u32 k = 0; k < EACH; ++k) {
-            if (value(sum0, same0) <= wanted && wanted < value(sum0 + part[k], same0 + same[k])) {
-                found[0] = threadIdx.x * EACH + k;
-                found64[0] = sum0;
-                found64[1] = same0;
+            for (u32 k = 0; k < EACH; ++k) {
+                if (any_of(part[k], same[k], m)) {
+                    end = threadIdx.x * EACH + k + 1;
+                    if (first == ~0u && value(s + part[k], m + same[k]) > wanted) first = end - 1;
+                }
+                s += part[k];
+                m += same[k];
             }
-            sum0 += part[k];
-            same0 += same[k];
+        }
+        find_ends(first, end);
+        __syncthreads();
+        const u32 at = min(min(found[0], found[1] - 1), n - 1);
+        if (threadIdx.x == at / EACH) {
+#pragma unroll
+            for (u32 k = 0; k < EACH; ++k)
+                if (k < at % EACH) sum0 += part[k], same0 += same[k];
+            found_sum = sum0;
+            found_count = same0;
         }
         __syncthreads();
-        const u32 at = min(found[0], n - 1);
-        const u64 sum1 = found64[0], same1 = found64[1];
+        const double sum1 = found_sum;
+        const u32 same1 = found_count;
         __syncthreads();
         if (wave == at % WAVES) {
             const u32 r = at / WAVES;
             Pack<T, V> x = fetch(r);
             cut(r, x);
-            u64 part[V], sum = 0;
+            double part[V], sum = 0.0;
             u32 same[V], sames = 0;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float l = (float)x.v[i];
                 const bool in = l >= last && some(l);
-                part[i] = in && (!TIES || l > last) ? amount(l) : 0;
+                part[i] = in && (!TIES || l > last) ? amount(l) : 0.0;
                 same[i] = TIES && in && l == last;
                 sum += part[i];
                 sames += same[i];
             }
-            u64 s = sum1 + scan_wave(sum) - sum, m = same1 + scan_wave(sames) - sames;
+            double s = sum1 + (scan_wave(sum) - sum);
+            u32 m = TIES ? same1 + scan_wave(sames) - sames : 0;
+            int hit = -1, latest = -1;
+            double hit_amount = 0.0, latest_amount = 0.0;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const u64 before = value(s, m), after = value(s + part[i], m + same[i]);
-                if (before <= wanted && wanted < after) {
-                    found[1] = at_of(r) + i;
-                    found64[0] = after - before;
+                if (any_of(part[i], same[i], m)) {
+                    latest = i;
+                    latest_amount = same[i] ? one : part[i];
+                    if (hit < 0 && value(s + part[i], m + same[i]) > wanted) hit = i, hit_amount = latest_amount;
                 }
                 s += part[i];
                 m += same[i];
             }
+            const u64 hits = __ballot(hit >= 0), some_here = __ballot(latest >= 0);
+            const u32 chosen = hits ? (u32)__ffsll((unsigned long long)hits) - 1 : 63 - (u32)__clzll((long long)(some_here | 1));
+            if (lane == chosen) {
+                found[2] = at_of(r) + (hits ? hit : max(latest, 0));
+                found_sum = hits ? hit_amount : latest_amount;
+            }
         }
         __syncthreads();
-        prob = (double)found64[0] / (double)all;
-        return found[1];
+        prob = found_sum / all;
+        return found[2];
     };
     constexpr std::integral_constant<int, 0> SPARSE;
     constexpr std::integral_constant<int, 1> MOST;
@@ -326,10 +421,6 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
 
     u64 *const list = mass, *const weight = mass + LISTED;  // tokens by their order: key, then the lower id; weights by rank
     auto entry = [](u32 id, float l) { return (u64)key_of(l) << 32 | (u32)~id; };
-    // Few lanes at a time have a token for the list: each adds 1 for itself.  (An address that the compiler knows to be one for all
-    // lanes makes it sum over the wave first, which takes ten times as long.)
-    u32 zero = 0;
-    asm volatile("" : "+v"(zero));
     auto enlist = [&](u32 id, float l) {
         const u32 at = atomicAdd(&n_list + zero, 1u);
         if (at < LISTED) list[at] = entry(id, l);
@@ -381,15 +472,15 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         last = top;
         const bool first = temperature <= 0.0f;
         const u32 id = draw(
-            SPARSE, [&](float) { return true; }, [&](float) { return 0ull; }, 1,
-            [&](u64 n) {
-                if (limit_k) n = min(n, (u64)top_k);
-                if (limit_p) n = (u64)fmax(ceil((double)top_p * (double)n), 1.0);
-                ties = first ? 1 : n;
-                return share(ties);
+            SPARSE, [&](float) { return true; }, [&](float) { return 0.0; }, 1.0,
+            [&](double n) {
+                if (limit_k) n = fmin(n, (double)top_k);
+                if (limit_p) n = fmax(ceil((double)top_p * n), 1.0);
+                ties = first ? 1 : (u32)n;
+                return share((double)ties);
             },
             prob);
-        return finish(id, ties == ~0ull ? 1.0 : 1.0 / (double)ties);
+        return finish(id, 1.0 / (double)ties);
     }
 
     if (limit_k && (u32)top_k <= LIST_K) {
@@ -416,7 +507,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
             u32 n[PER], sum = 0;
 #pragma unroll
             for (int k = 0; k < PER; ++k) sum += n[k] = count[PER * threadIdx.x + k];
-            u32 upto = (u32)scan_block(sum) - sum;
+            u32 all, upto = scan_counts(sum, all) - sum;
             if (threadIdx.x == 0) found[0] = BINS - 1, n_list = 0;
             __syncthreads();
 #pragma unroll
@@ -437,68 +528,31 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
         }
         if (listed <= LISTED) {
             sort_list(listed);
-            // consecutive ranks a thread
-            constexpr u32 EACH = 1;
-            const u32 kept = min((u32)top_k, listed);
-            u64 w[EACH], sum = 0;
-            u32 id[EACH];
-#pragma unroll
-            for (u32 k = 0; k < EACH; ++k) {
-                const u32 rank = threadIdx.x * EACH + k;
-                const u64 at = rank < kept ? list[rank] : 0;
-                id[k] = ~(u32)at;
-                const Weight x = weigh(value_of((u32)(at >> 32)));
-                w[k] = rank < kept && x.w >= least ? whole(x.w) : 0;
-                // top_p goes by all of them, whatever min_p leaves
-                sum += rank < kept ? whole(x.w) : 0;
-            }
-            u64 before = scan_block(sum);
-            if (threadIdx.x == THREADS - 1) found64[0] = before;
-            before -= sum;
-            __syncthreads();
-            const double limit = limit_p ? fmax((double)top_p * (double)found64[0], 0.5) : __builtin_inf();
-            sum = 0;
-#pragma unroll
-            for (u32 k = 0; k < EACH; ++k) {
-                const u32 rank = threadIdx.x * EACH + k;
-                const u64 own = rank < kept ? whole(weigh(value_of((u32)(list[rank] >> 32))).w) : 0;
-                if (!((double)before < limit)) w[k] = 0;
-                before += own;
-                sum += w[k];
-                if (rank < kept) weight[rank] = w[k];
-            }
-            __syncthreads();
+            // a rank a thread
+            const u32 kept = min((u32)top_k, listed), rank = threadIdx.x;
+            const u64 own = rank < kept ? list[rank] : 0;
+            const float l = value_of((u32)(own >> 32));
+            const double w = rank < kept ? weigh(l).w : 0.0;
+            // top_p goes by all of them, whatever min_p leaves
+            double all, before = scan_sums(w, all) - w;
+            const double limit = limit_p ? fmax((double)top_p * all, TINY) : __builtin_inf();
+            if (rank < kept) weight[rank] = (u64)__double_as_longlong(before < limit && w >= least ? w : 0.0);
             // by ids
             u32 many = 64;
             while (many < kept) many *= 2;
-#pragma unroll
-            for (u32 k = 0; k < EACH; ++k) {
-                const u32 rank = threadIdx.x * EACH + k;
-                if (rank < many) list[rank] = rank < kept ? (u64)(u32)~id[k] << 32 | rank : 0;
-            }
+            __syncthreads();
+            if (rank < many) list[rank] = rank < kept ? (u64)(u32)own << 32 | rank : 0;
+            if (threadIdx.x == 0) found[0] = ~0u, found[1] = 0;
             __syncthreads();
             sort(many);
-            sum = 0;
-#pragma unroll
-            for (u32 k = 0; k < EACH; ++k) {
-                const u32 rank = threadIdx.x * EACH + k;
-                const u64 at = rank < kept ? list[rank] : 0;
-                id[k] = ~(u32)(at >> 32);
-                w[k] = rank < kept ? weight[(u32)at] : 0;
-                sum += w[k];
-            }
-            before = scan_block(sum);
-            if (threadIdx.x == THREADS - 1) found64[0] = before;
-            before -= sum;
+            const u64 at = rank < kept ? list[rank] : 0;
+            const double part = rank < kept ? __longlong_as_double((long long)weight[(u32)at]) : 0.0;
+            const double upto = scan_sums(part, all), wanted = share(all);
+            find_ends(part > 0.0 && upto > wanted ? rank : ~0u, part > 0.0 ? rank + 1 : 0);
             __syncthreads();
-            const u64 all = found64[0], wanted = share(all);
-#pragma unroll
-            for (u32 k = 0; k < EACH; ++k) {
-                if (before <= wanted && wanted < before + w[k]) {
-                    a.token[row] = (int32_t)id[k];
-                    if (a.prob) a.prob[row] = (float)((double)w[k] / (double)all);
-                }
-                before += w[k];
+            if (rank == min(found[0], found[1] - 1)) {
+                a.token[row] = (int32_t)~(u32)(at >> 32);
+                if (a.prob) a.prob[row] = (float)(part / all);
             }
             return;
         }
@@ -515,20 +569,25 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                 const float l = (float)x.v[i];
                 if (may(l)) {
                     const Weight w = weigh(l);
-                    if (w.n < GRAINS) {
-                        atomicAdd((unsigned long long *)&mass[bin_of(w.n)], (unsigned long long)whole(w.w));
-                        if (limit_k) atomicAdd(&count[bin_of(w.n)], 1u);
-                    }
+                    const u32 bin = bin_of(w.n);
+                    atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)whole(w.w, bin));
+                    if (limit_k) atomicAdd(&count[bin], 1u);
                 }
                 if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
         });
         __syncthreads();
-        struct Bins {  // the thread's: what is in each, and in all up to each
-            u64 mass[PER], upto_mass[PER];
-            u32 count[PER], upto_count[PER];
+        struct Bins {  // the thread's: what is in each, and in all before each and behind the last
+            u64 mass[PER];
+            u32 count[PER];
+            double upto_mass[PER + 1];
+            u32 upto_count[PER + 1];
         };
-        auto scan_bins = [&](u64 m0, u32 c0) {  // m0, c0: what lies above them
+        double total;
+        u32 tokens;
+        // m0, c0: what lies above them; bin: that which they are parts of, or ~0.  (A thread's lie in one octave: their sums are exact.)
+        static_assert(OCTAVE % PER == 0, "scan_bins");
+        auto scan_bins = [&](double m0, u32 c0, u32 bin, double &all, u32 &all_count) {
             Bins b;
             u64 m = 0;
             u32 n = 0;
@@ -537,50 +596,60 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                 b.mass[k] = mass[PER * threadIdx.x + k], b.count[k] = count[PER * threadIdx.x + k];
                 m += b.mass[k], n += b.count[k];
             }
-            m = m0 + scan_block(m) - m;
-            n = c0 + (u32)scan_block(n) - n;
+            const u32 octave = bin == ~0u ? PER * threadIdx.x : bin;
+            const double own = sum_of(m, octave);
+            double before = own;
+            u32 before_count = n;
+            scan_both(before, all, before_count, all_count);
+            before = m0 + (before - own), before_count = c0 + before_count - n;
+            m = 0, n = 0;
 #pragma unroll
-            for (int k = 0; k < PER; ++k) b.upto_mass[k] = m += b.mass[k], b.upto_count[k] = n += b.count[k];
+            for (int k = 0; k <= PER; ++k) {
+                b.upto_mass[k] = before + sum_of(m, octave), b.upto_count[k] = before_count + n;
+                if (k < PER) m += b.mass[k], n += b.count[k];
+            }
             return b;
         };
-        const Bins bins = scan_bins(0, 0);
-        if (threadIdx.x == THREADS - 1) {
-            found64[0] = bins.upto_mass[PER - 1];
-            found[0] = bins.upto_count[PER - 1];
-        }
-        __syncthreads();
-        u64 total = found64[0];
-        const u32 tokens = found[0];
+        const Bins bins = scan_bins(0.0, 0, ~0u, total, tokens);
         // Narrows to the last token that counts: with `by_count` the goal_count-th, else the one before which weights sum to less than
         // goal_mass and with which they do not.  Lowers the tokens kept to those up to it; returns the weights up to and with it.
-        auto resolve = [&](bool by_count, u64 goal_count, double goal_mass) -> u64 {
-            const auto reached = [&](u64 n, u64 m) { return by_count ? n >= goal_count : (double)m >= goal_mass; };
-            const auto lower = [&](float l, u64 n) {
+        auto resolve = [&](bool by_count, u32 goal_count, double goal_mass) -> double {
+            const auto reached = [&](u32 n, double m) { return by_count ? n >= goal_count : m >= goal_mass; };
+            const auto lower = [&](float l, u32 n) {
                 if (l > last)
                     last = l, ties = n;
                 else if (l == last)
                     ties = min(ties, n);
             };
-            auto find = [&](const Bins &b) {
+            // The first bin with which it is reached, and what lies above it; if none is: ~0, or with `inner` (parts of a bin with which
+            // it is, but for a rounding) the last that holds something.
+            auto find = [&](const Bins &b, bool inner) {
                 __syncthreads();
-                if (threadIdx.x == 0) found[0] = ~0u;
+                if (threadIdx.x == 0) found[0] = ~0u, found[1] = 0;
                 __syncthreads();
+                u32 first = ~0u, end = 0;
 #pragma unroll
-                for (int k = 0; k < PER; ++k) {
-                    const u32 n = b.upto_count[k] - b.count[k];
-                    const u64 m = b.upto_mass[k] - b.mass[k];
-                    if (reached(b.upto_count[k], b.upto_mass[k]) && !reached(n, m)) {
-                        found[0] = PER * threadIdx.x + k;
-                        found[1] = n;
-                        found64[0] = m;
+                for (int k = 0; k < PER; ++k)
+                    if (by_count ? b.count[k] != 0 : b.mass[k] != 0) {
+                        end = PER * threadIdx.x + k + 1;
+                        if (first == ~0u && reached(b.upto_count[k + 1], b.upto_mass[k + 1])) first = end - 1;
                     }
-                }
+                find_ends(first, inner ? end : 0);
                 __syncthreads();
+                const u32 bin = inner ? min(found[0], found[1] - 1) : found[0];
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (PER * threadIdx.x + k == bin) {
+                        found_count = b.upto_count[k];
+                        found_sum = b.upto_mass[k];
+                    }
+                __syncthreads();
+                return bin;
             };
-            find(bins);
-            const u32 bin = found[0];
-            u64 above_count = found[1], above_mass = found64[0];
+            const u32 bin = find(bins, false);
             if (bin == ~0u) return total;  // all of them count
+            u32 above_count = found_count;
+            double above_mass = found_sum;
             // logits of the bin, and a little beside it
             float lo = fmaxf((float)(top64 - ((bin + 1) * (GRAINS / BINS) + 0.5) / c) - reach, floor_l), hi = (float)(top64 - (bin * (GRAINS / BINS) - 1.0) / c) + reach;
             if (!(c > 0.0)) lo = floor_l, hi = top;
@@ -629,51 +698,48 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                     });
                 }
                 if (mine) {
-                    atomicMin(&key_min, low);
-                    atomicMax(&key_max, high);
-                    atomicAdd(&n_bin, mine);
+                    atomicMin(&key_min + zero, low);
+                    atomicMax(&key_max + zero, high);
+                    atomicAdd(&n_bin + zero, mine);
                 }
                 __syncthreads();
                 const u32 members = n_bin;
                 from = key_min, to = key_max;
                 if (from == to) {  // equal ones: so many of them
                     const float l = value_of(from);
-                    const u64 w = whole(weigh(l).w);
-                    u64 m;
-                    if (by_count) {
-                        m = goal_count - above_count;
-                    } else {  // the smallest m with above + m w >= goal
-                        m = w ? (u64)((goal_mass - (double)above_mass) / (double)w) : 1;
-                        while (m > 1 && (double)(above_mass + (m - 1) * w) >= goal_mass) --m;
-                        while (m < members && (double)(above_mass + m * w) < goal_mass) ++m;
-                    }
-                    m = min(max(m, 1ull), (u64)members);
-                    lower(l, m);
-                    return above_mass + m * w;
+                    const double w = weigh(l).w;
+                    // the smallest m with above + m w >= goal
+                    const double m = by_count ? (double)(goal_count - above_count) : ceil((goal_mass - above_mass) / w);
+                    const u32 n = (u32)fmin(fmax(m, 1.0), (double)members);
+                    lower(l, n);
+                    return above_mass + n * w;
                 }
                 if (fits) {  // in their order
+                    if (threadIdx.x == 0) found[0] = ~0u;
                     sort_list(n);
                     constexpr u32 EACH = LISTED / THREADS;
-                    u64 w[EACH], m = 0;
+                    double w[EACH], m = 0.0;
 #pragma unroll
                     for (u32 k = 0; k < EACH; ++k) {
                         const u32 rank = threadIdx.x * EACH + k;
-                        m += w[k] = rank < members ? whole(weigh(value_of((u32)(list[rank] >> 32))).w) : 0;
+                        m += w[k] = rank < members ? weigh(value_of((u32)(list[rank] >> 32))).w : 0.0;
                     }
-                    u64 before = above_mass + scan_block(m) - m;
+                    double all, upto[EACH], sum = above_mass + (scan_sums(m, all) - m);
+                    u32 hit = ~0u;
 #pragma unroll
                     for (u32 k = 0; k < EACH; ++k) {
                         const u32 rank = threadIdx.x * EACH + k;
-                        const u64 at = above_count + rank;
-                        if (rank < members && !reached(at, before) && reached(at + 1, before + w[k])) {
-                            found[2] = rank;
-                            found64[1] = before + w[k];
-                        }
-                        before += w[k];
+                        upto[k] = sum += w[k];
+                        if (hit == ~0u && rank < members && reached(above_count + rank + 1, sum)) hit = rank;
                     }
+                    find_ends(hit, 0);
+                    __syncthreads();
+                    const u32 rank = min(found[0], members - 1), key = (u32)(list[rank] >> 32);
+#pragma unroll
+                    for (u32 k = 0; k < EACH; ++k)
+                        if (threadIdx.x * EACH + k == rank) found_sum = upto[k];
                     __syncthreads();
                     // its place among its equals: the first of them by halves
-                    const u32 rank = min(found[2], members - 1), key = (u32)(list[rank] >> 32);
                     u32 first = 0, end = rank;
                     while (first < end) {
                         const u32 mid = (first + end) / 2;
@@ -683,7 +749,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                             end = mid;
                     }
                     lower(value_of(key), rank - first + 1);
-                    return found64[1];
+                    return found_sum;
                 }
                 // by bins of their keys
                 u32 shift = 0;
@@ -694,54 +760,53 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
                     const u32 key = key_of(l);
                     const Weight w = weigh(l);
                     if (bin_of(w.n) != bin || key < from || key > to) return;
-                    atomicAdd((unsigned long long *)&mass[(to - key) >> shift], (unsigned long long)whole(w.w));
+                    atomicAdd((unsigned long long *)&mass[(to - key) >> shift], (unsigned long long)whole(w.w, bin));
                     atomicAdd(&count[(to - key) >> shift], 1u);
                 });
                 __syncthreads();
-                find(scan_bins(above_mass, (u32)above_count));
-                above_count = found[1];
-                above_mass = found64[0];
-                to -= min(found[0], BINS - 1) << shift;
+                double all;
+                u32 all_count;
+                const u32 part = min(find(scan_bins(above_mass, above_count, bin, all, all_count), true), BINS - 1);
+                above_count = found_count;
+                above_mass = found_sum;
+                to -= part << shift;
                 const u32 width = (1u << shift) - 1;
                 from = to - from > width ? to - width : from;
             }
         };
         // No more tokens and weights than these reach min_p: a limit that they keep to leaves them all.
-        u64 likely_mass = ~0ull;
+        double likely_mass = __builtin_inf();
         u32 likely = ~0u;
         if (least > 0.0) {
-            // (the logarithm of the hardware takes a subnormal as 0; and no weight is below 2^-64)
-            const u32 bin = min(bin_of((u32)(-__log2f(fmaxf((float)least, 0x1p-64f)) * GRAIN) + 3), BINS - 1);
+            const u32 bin = bin_of((u32)(-least_log * GRAIN) + 3);
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < PER; ++k)
-                if (PER * threadIdx.x + k == bin) found64[0] = bins.upto_mass[k], found[0] = bins.upto_count[k];
+                if (PER * threadIdx.x + k == bin) found_sum = bins.upto_mass[k + 1], found[0] = bins.upto_count[k + 1];
             __syncthreads();
-            likely_mass = found64[0];
+            likely_mass = found_sum;
             likely = found[0];
         }
         // (Where top_p follows, it goes by the sum of the top_k.)
-        if (limit_k && (u32)top_k < (limit_p ? tokens : min(tokens, likely))) total = resolve(true, (u64)top_k, 0.0);
-        const double goal = fmax((double)top_p * (double)total, 0.5);
-        if (limit_p && !((double)likely_mass <= goal)) resolve(false, 0, goal);
+        if (limit_k && (u32)top_k < (limit_p ? tokens : min(tokens, likely))) total = resolve(true, (u32)top_k, 0.0);
+        const double goal = fmax((double)top_p * total, TINY);
+        if (limit_p && !(likely_mass <= goal)) resolve(false, 0, goal);
     }
+    const double w_last = weigh(last).w, one = w_last >= least ? w_last : 0.0;
+    const auto weight_of = [&](float l) { return weigh(l).w; };
     u32 id;
-    const double w_last = weigh(last).w;
-    const u64 one = w_last >= least ? whole(w_last) : 0ull;
-    if (least > 0.0 || (!many && (last > floor_l || ties != ~0ull))) {
-        // logits that may reach min_p, and a little below
-        const float enough = least > 0.0 ? (float)(top64 + (__log2f(fmaxf((float)least, 0x1p-64f)) * GRAIN - 1.0) / c) - reach : last;
+    if (least > 0.0 || (!many && (last > floor_l || ties != ~0u))) {
         id = draw(
-            SPARSE, [&](float l) { return !(l < enough); },
-            [&](float l) -> u64 {
+            SPARSE, [&](float l) { return l >= enough; },
+            [&](float l) {
                 const double w = weigh(l).w;
-                return w >= least ? whole(w) : 0ull;
+                return w >= least ? w : 0.0;
             },
             one, share, prob);
-    } else if (last > floor_l || ties != ~0ull) {
-        id = draw(MOST, may, [&](float l) { return whole(weigh(l).w); }, one, share, prob);
+    } else if (last > floor_l || ties != ~0u) {
+        id = draw(MOST, may, weight_of, one, share, prob);
     } else {
-        id = draw(ALL, may, [&](float l) { return whole(weigh(l).w); }, 0, share, prob);
+        id = draw(ALL, may, weight_of, 0.0, share, prob);
     }
     finish(id, prob);
 }

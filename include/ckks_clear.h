@@ -179,7 +179,8 @@ typedef struct {
  *   with d_k_norm (d_q_norm), [head_dim] of norm_dtype (F32 or dtype):  x = x / sqrt(mean(x^2) + eps) * weight over each head's entries
  *   rotation as in ckks_clear_cache_append
  *   each block of 32 entries: e = the smallest number >= -100 with max |x| <= M 2^e, M = 448 (E4M3) or 127 (I8),
- *   power = e + 127, codes = x / 2^e rounded to the nearest, ties to even.
+ *   power = e + 127, codes = x / 2^e rounded to the nearest, ties to even; of a block that dtype holds, to the nearest whose value it
+ *   holds too (finite entries up to the type's largest stay finite).
  * A block that holds an infinity, a NaN or an entry of 2^128 or more is stored as power 255 and codes 0.  Norm and rotation are
  * computed in 64 bits; keys meet no other rounding than that to their code, queries are rounded to 32 bits and to dtype.
  * Rotated entries without an angle are NaN, and so is, in the cache, their block.  What is not stored, what may lie in what, rows in
@@ -217,7 +218,8 @@ int ckks_clear_packed_attend(const ckks_clear_packed_attend_t *a, void *stream);
 
 /* Reads the new tokens' keys and values (all of a sequence's, if as many rows as kv_len are asked for) back: the values that the codes
  * stand for, in dtype.  A token at a position below 0 or in a page outside [0, n_pages) reads as zeros; rows in no sequence
- * are not written.  Rows that ckks_clear_packed_append wrote give the same values when they are read and appended again.
+ * are not written.  Rows that ckks_clear_packed_append wrote give the same values when they are read and appended again, in F16 where it
+ * holds them: its largest number is 65504, which normed keys may pass, and it rounds small ones to multiples of 2^-24.
  * d_k_out, d_v_out [n_tokens][kv_heads][head_dim] by strides {token, head}, either NULL; they share no entry. */
 typedef struct {
     ckks_clear_packed_t pages;

@@ -112,9 +112,19 @@ __device__ __forceinline__ double rsqrt_of(double x) {
     return x < __builtin_inf() ? r : y;  // infinity: 0
 }
 
+// Blocks whose entries T holds end below TOP (as T rounds, where that is still to be done).  Of those above HIGH, with their last power, a code
+// of 256 or 64 stands for 2^16 (F16) or 2^128, which T does not hold; the one before it is right.
+template <class T, int FORM>
+struct Range {
+    static constexpr bool F = std::is_same<T, f16>::value;
+    static constexpr float TOP = F ? 65520.0f : __builtin_inff();
+    static constexpr float HIGH = FORM == E4M3 ? (F ? 448 * 0x1p7f : 448 * 0x1p119f) : (F ? 127 * 0x1p9f : 127 * 0x1p121f);
+};
+
 // Eight entries of a block of 32 spread over four lanes, as codes; `power` is the block's.
-template <int FORM>
+template <class T, int FORM>
 __device__ __forceinline__ uint2 pack8(const float *x, u32 &power) {
+    typedef Range<T, FORM> range;
     u32 top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
@@ -124,6 +134,7 @@ __device__ __forceinline__ uint2 pack8(const float *x, u32 &power) {
     const u32 e = (top >> 23) + ((top & 0x7fffffu) > MANTISSA);
     power = top >= 0x7f800000u ? 255u : max(e, LEAST + SHIFT) - SHIFT;
     const float f = __uint_as_float((254 - min(power, 253u)) << 23);
+    const bool high = top > __builtin_bit_cast(u32, range::HIGH) && top < __builtin_bit_cast(u32, range::TOP);
     uint2 r;
     if (FORM == E4M3) {
         int lo = 0, hi = 0;
@@ -132,10 +143,21 @@ __device__ __forceinline__ uint2 pack8(const float *x, u32 &power) {
         hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4] * f, x[5] * f, hi, false);
         hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6] * f, x[7] * f, hi, true);
         r = make_uint2((u32)lo, (u32)hi);
+        if (__any(high))
+            if (high) {
+                // 0x78 is the last code that such a block has; bit 7 of a byte of y is set where it is
+                auto before = [](u32 w) {
+                    const u32 y = 0x80808080u - ((w & 0x7f7f7f7fu) ^ 0x78787878u);
+                    return w - ((y & 0x80808080u) >> 7);
+                };
+                r = make_uint2(before(r.x), before(r.y));
+            }
     } else {
+        // x 2^-e is exact, and its sum with 1.5 2^23 is rounded to a whole number, whose lowest bits are the code
+        const float end = high ? 63.0f : 127.0f;
         u32 c[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i] = (u32)(int)__builtin_rintf(x[i] * f) & 0xffu;
+        for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(__builtin_amdgcn_fmed3f(x[i] * f, -end, end) + 12582912.0f) & 0xffu;
         r = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
     }
     if (power == 255) r = make_uint2(0, 0);
@@ -189,7 +211,7 @@ __global__ __launch_bounds__(256, 4) void packed_append_kernel(PackedAppendArgs 
     };
     auto store_codes = [&](const float *x, unsigned char *codes, unsigned char *powers) {
         u32 power;
-        const uint2 packed = pack8<FORM>(x, power);
+        const uint2 packed = pack8<T, FORM>(x, power);
         if (live) {
             __builtin_memcpy(codes + c, &packed, 8);
             if (c % PACK_BLOCK == 0) powers[c / PACK_BLOCK] = (unsigned char)power;

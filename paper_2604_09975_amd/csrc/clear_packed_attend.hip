@@ -213,6 +213,8 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
     u32 odd = 0;
     C *vb = (C *)lds + kw * TK * VS;
 
+    // The largest power with which every code that is a number is finite.
+    constexpr u32 LARGE = std::is_same<C, f16>::value ? (FORM == E4M3 ? 127 + 7 : 127 + 8) : (FORM == E4M3 ? 127 + 119 : 127 + 120);
     auto k_power = [&](float power, int h) { return full || k_ok[h] ? power : 1.0f; };
     auto score = [&](Tile &x) {
         if (!full)  // what a lane has beyond the head
@@ -222,33 +224,47 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
                 for (int h = 0; h < KP; ++h)
                     if (!k_ok[h]) x.k[u][h] = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < 2; ++u)
             if (__any(x.none & 3u))
                 if (x.none >> u & 1) {
 #pragma unroll
                     for (int h = 0; h < KP; ++h) x.k[u][h] = make_uint4(0, 0, 0, 0);
                     x.kz[u] = 0;
                 }
-            const float power = power_of<FORM>(x.kz[u]);
+        auto products = [&](auto finite) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[u][i] = 0.0f;
+            for (int u = 0; u < 2; ++u) {
+                const float power = power_of<FORM>(x.kz[u]);
 #pragma unroll
-            for (int d = 0; d < STEPS; ++d) {
-                C k[8];
-                const uint4 y = x.k[u][d / 2];
-                unpack4<C, FORM>(d % 2 ? y.z : y.x, k_power(power, d / 2), k);
-                unpack4<C, FORM>(d % 2 ? y.w : y.y, k_power(power, d / 2), k + 4);
-                frag f;
-                __builtin_memcpy(&f, k, 16);
+                for (int i = 0; i < 4; ++i) s[u][i] = 0.0f;
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) s[u] = mma16(f, qf[n][d], s[u]);
+                for (int d = 0; d < STEPS; ++d) {
+                    C k[8];
+                    const uint4 y = x.k[u][d / 2];
+                    unpack4<C, FORM>(d % 2 ? y.z : y.x, k_power(power, d / 2), k);
+                    unpack4<C, FORM>(d % 2 ? y.w : y.y, k_power(power, d / 2), k + 4);
+                    frag f;
+                    __builtin_memcpy(&f, k, 16);
+                    s[u] = mma16(f, qf[0][d], s[u]);
+                    if (decltype(finite)::value) {
+                        uint4 z;
+                        u32 odd_key = 0;
+                        __builtin_memcpy(&z, k, 16);
+                        z = finite_part<C>(z, odd_key);
+                        __builtin_memcpy(&f, &z, 16);
+                    }
+#pragma unroll
+                    for (int n = 1; n < NQ; ++n) s[u] = mma16(f, qf[n][d], s[u]);
+                }
             }
-        }
+        };
+        products(std::false_type());
+        // an infinite key is for the query's first part alone: the others may be 0
+        if (NQ > 1 && __any(max(x.kz[0], x.kz[1]) > LARGE)) products(std::true_type());
     };
     // An infinity or NaN among the values would meet weights of 0, and here also the rest of a weight, which may be: such values are taken as
     // zeros and come back at the end.  Only large powers give one (and codes that are no number, which matter where some row does not
     // see the tile in full).
-    constexpr u32 LARGE = std::is_same<C, f16>::value ? (FORM == E4M3 ? 127 + 7 : 127 + 8) : (FORM == E4M3 ? 127 + 119 : 127 + 120);
     auto put_v = [&](u32 tile, Tile &x) {
         const int j0 = (int)((r.tile0 + tile) * TK);
         u32 large = 0;

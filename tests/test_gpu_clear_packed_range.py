@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from tests.clear_util import TYPES, gen, randn
+from tests.clear_util import TINY, TYPES, U, close, gen, randn
 from tests.packed_util import FORMATS, LARGEST, PackedCache, code_values, same, values
 
 pytestmark = pytest.mark.gpu
@@ -90,3 +90,32 @@ def test_rows_read_and_appended_again_wherever_the_type_holds_them(dtype, form):
     assert exact.sum() > n // 4
     for a, b in zip(got, twice):
         assert torch.equal(a.double()[exact.expand_as(a)], held[exact.expand_as(a)]) and torch.equal(a[exact.expand_as(a)], b[exact.expand_as(a)])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("lens,heads,dim", [([(1, 70), (2, 40)], 4, 64), ([(1, 300)], 16, 128), ([(90, 130)], 8, 128), ([(1, 50)], 2, 72)])
+def test_infinite_keys(lens, heads, dim, dtype):
+    """A code may stand for more than the type holds.  A key that is infinite there gives a score that is: below all others it
+    has no weight, above them it leaves the row no number, as over a plain cache."""
+    from paper_2604_09975_amd import clear as K
+    dtype = TYPES[dtype]
+    c = PackedCache(lens, heads, 2, dim, 16, dtype, 7, torch.int8)
+    c.q[:, :, 5] = torch.where(torch.arange(heads, device="cuda") % 2 == 0, 1.0, -1.5).to(dtype)  # signs of the scores, by heads
+    pg = int(c.table[0, 1])
+    z = 127 + (10 if dtype is torch.float16 else 122)
+    c.power[0][pg, 0, 3] = z
+    c.codes[0][pg, 0, 3] = 0
+    c.codes[0][pg, 0, 3, 5] = 100  # the 20th key of the first kv head's queries
+    out = K.ckks_clear_packed_attend(c.q, *c.args())
+    c.refresh()
+    plain = [x.to(dtype) for x in (c.k, c.v)]
+    assert torch.isinf(plain[0][pg, 0, 3, 5]) and int(torch.isinf(plain[0]).sum()) == 1
+    want = K.ckks_clear_attend(c.q, *plain, c.page_table, c.q_start, c.kv_len)
+    n, kv = c.lens[0]
+    sees = torch.arange(kv - n, kv, device="cuda") >= 19
+    first = torch.arange(heads, device="cuda") < heads // 2
+    up = torch.arange(heads, device="cuda") % 2 == 0
+    assert torch.isnan(want[:n][sees][:, first & up]).all() and torch.isfinite(want[:n][:, first & ~up]).all()
+    # either result: weights rounded (twice U of the sum of weight times value), the result rounded once, 2^-13 of that sum for scores in 32 bits
+    mass = K.ckks_clear_attend(c.q, plain[0], plain[1].abs(), c.page_table, c.q_start, c.kv_len).double()
+    close(out, want.double(), 2 * (3 * U[dtype] + 2.0**-13) * 1.01 * mass.nan_to_num() + TINY[dtype])

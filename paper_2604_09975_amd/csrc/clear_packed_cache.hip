@@ -26,7 +26,7 @@ struct PackedAppendArgs {
     const void *k_norm, *q_norm;
     const float *cos, *sin;
     const int32_t *positions, *q_start, *kv_len, *table;
-    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, head_dim, rot, n_pos, interleaved, norm_f32, slices, kinds;
+    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, heads, head_dim, rot, n_pos, interleaved, norm_f32, slices, kinds, t0;
     double eps, inv_dim;
 };
 
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(256, 4) void packed_append_kernel(PackedAppendArgs 
             weights[k][i] = !norm || i >= a.head_dim ? 1.0f : a.norm_f32 ? ((const float *)norm)[i] : (float)((const T *)norm)[i];
     }
     __syncthreads();
-    const u32 t = blockIdx.x * 4 + wave, kinds = a.kinds, only = blockIdx.y % kinds, slice = blockIdx.y / kinds;
+    const u32 t = a.t0 + blockIdx.x * 4 + wave, kinds = a.kinds, only = blockIdx.y % kinds, slice = blockIdx.y / kinds;
     if (t >= a.n_tokens) return;
     const u32 first = slice * GROUPS + lane / G, step = a.slices * GROUPS;  // heads of the group
     const u32 c = lane % G * 8, dim = a.head_dim, rot = a.rot, half = rot / 2;
@@ -371,7 +371,7 @@ struct PackedReadArgs {
     void *ko, *vo;
     i64 pks[3], pvs[3], zks[3], zvs[3], kos[2], vos[2], ts;
     const int32_t *q_start, *kv_len, *table;
-    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, head_dim, slices;
+    u32 n_seq, n_tokens, n_pages, page_size, table_width, kv_heads, head_dim, slices, t0;
 };
 
 // A wave takes a token, a lane eight entries.  Bound by memory: 101 thousand tokens of 8 heads of 128 (214 MB) as bf16
@@ -380,7 +380,7 @@ template <class T, int FORM>
 __global__ __launch_bounds__(256) void packed_read_kernel(PackedReadArgs a) {
     const u32 lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const u64 job = (u64)blockIdx.x * 4 + wave;
-    const u32 t = (u32)(job / a.slices), slice = (u32)(job % a.slices);
+    const u32 t = a.t0 + (u32)(job / a.slices), slice = (u32)(job % a.slices);
     if (t >= a.n_tokens) return;
     const TokenPlace at = place_of(a, t);
     if (at.pos == -2) return;
@@ -408,14 +408,18 @@ __global__ __launch_bounds__(256) void packed_read_kernel(PackedReadArgs a) {
 }
 
 // Waves of a token: enough to fill the CUs where there are few tokens, at most one for each turn of its work.
+// (a launch has fewer than 2^32 threads: tokens of one)
+constexpr u32 TOKENS = 1u << 25;
 static u32 slices_of(u32 n_tokens, u32 turns) { return std::max(1u, std::min(turns, 4096 / std::max(n_tokens, 1u))); }
 
 template <class T, int FORM, int G>
 static int launch_packed_append(PackedAppendArgs a, hipStream_t st) {
     a.slices = slices_of(a.n_tokens, (std::max(a.kv_heads, a.heads) + 64 / G - 1) / (64 / G));
     a.kinds = a.n_tokens * a.slices <= 2048 ? 3 : 1;
-    hipLaunchKernelGGL((packed_append_kernel<T, FORM, G>), dim3((a.n_tokens + 3) / 4, a.slices * a.kinds), dim3(256), 0, st, a);
-    CKKS_LAUNCH_CHECK("packed_append_kernel");
+    for (; a.t0 < a.n_tokens; a.t0 += TOKENS) {
+        hipLaunchKernelGGL((packed_append_kernel<T, FORM, G>), dim3((std::min(a.n_tokens - a.t0, TOKENS) + 3) / 4, a.slices * a.kinds), dim3(256), 0, st, a);
+        CKKS_LAUNCH_CHECK("packed_append_kernel");
+    }
     return CKKS_OK;
 }
 template <class T, int FORM>
@@ -432,12 +436,14 @@ static int launch_packed_append(const PackedAppendArgs &a, u32 format, hipStream
 template <class T>
 static int launch_packed_read(PackedReadArgs a, u32 format, hipStream_t st) {
     a.slices = slices_of(a.n_tokens, (2 * a.kv_heads * (a.head_dim / 8) + 63) / 64);
-    const u64 blocks = ((u64)a.n_tokens * a.slices + 3) / 4;
-    if (format == CKKS_CLEAR_E4M3)
-        hipLaunchKernelGGL((packed_read_kernel<T, E4M3>), dim3((u32)blocks), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((packed_read_kernel<T, I8>), dim3((u32)blocks), dim3(256), 0, st, a);
-    CKKS_LAUNCH_CHECK("packed_read_kernel");
+    for (; a.t0 < a.n_tokens; a.t0 += TOKENS) {
+        const u32 blocks = (std::min(a.n_tokens - a.t0, TOKENS) * a.slices + 3) / 4;
+        if (format == CKKS_CLEAR_E4M3)
+            hipLaunchKernelGGL((packed_read_kernel<T, E4M3>), dim3(blocks), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((packed_read_kernel<T, I8>), dim3(blocks), dim3(256), 0, st, a);
+        CKKS_LAUNCH_CHECK("packed_read_kernel");
+    }
     return CKKS_OK;
 }
 

@@ -39,7 +39,7 @@ struct SampleArgs {
     const float *u, *temperature, *top_p, *min_p;
     const int32_t *top_k;
     i64 stride;
-    u32 vocab, bits;
+    u32 vocab, bits, row0;
 };
 
 // Inclusive sums over the lanes of a wave: by DPP within rows of 16, then from row to row.
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     __shared__ double found_sum;
     __shared__ float wave_top[WAVES];
 
-    const u32 row = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32 row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const T *in = (const T *)a.logits + (i64)row * a.stride;
     const u32 rounds = (a.vocab + SPAN - 1) / SPAN;
     // First id of the thread's part of a round; the last ones of a row begin before their place, and what lies there is left out.
@@ -812,14 +812,19 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
 }
 
 template <class T>
-static void launch_sample(const SampleArgs &a, u32 rows, hipStream_t st) {
-    constexpr u32 V = 8;
-    if (a.vocab < V)
-        hipLaunchKernelGGL((sample_kernel<T, 256, 1>), dim3(rows), dim3(256), 0, st, a);
-    else if (a.vocab <= 256 * V * 4)
-        hipLaunchKernelGGL((sample_kernel<T, 256, V>), dim3(rows), dim3(256), 0, st, a);
-    else
-        hipLaunchKernelGGL((sample_kernel<T, 1024, V>), dim3(rows), dim3(1024), 0, st, a);
+static int launch_sample(SampleArgs a, u32 rows, hipStream_t st) {
+    constexpr u32 V = 8, ROWS = 1u << 21;  // rows of a launch, which has fewer than 2^32 threads
+    for (; a.row0 < rows; a.row0 += ROWS) {
+        const u32 n = std::min(rows - a.row0, ROWS);
+        if (a.vocab < V)
+            hipLaunchKernelGGL((sample_kernel<T, 256, 1>), dim3(n), dim3(256), 0, st, a);
+        else if (a.vocab <= 256 * V * 4)
+            hipLaunchKernelGGL((sample_kernel<T, 256, V>), dim3(n), dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL((sample_kernel<T, 1024, V>), dim3(n), dim3(1024), 0, st, a);
+        CKKS_LAUNCH_CHECK("sample_kernel");
+    }
+    return CKKS_OK;
 }
 
 }  // namespace ckks
@@ -860,12 +865,7 @@ extern "C" int ckks_clear_sample(const ckks_clear_sample_t *p, void *stream) {
     while ((1u << (62 - a.bits)) < p->vocab) --a.bits;
     a.bits = std::min(a.bits, 51u);
     hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == CKKS_CLEAR_F32)
-        launch_sample<float>(a, n, st);
-    else if (p->dtype == CKKS_CLEAR_F16)
-        launch_sample<f16>(a, n, st);
-    else
-        launch_sample<bf16>(a, n, st);
-    CKKS_LAUNCH_CHECK("sample_kernel");
-    return CKKS_OK;
+    return p->dtype == CKKS_CLEAR_F32   ? launch_sample<float>(a, n, st)
+           : p->dtype == CKKS_CLEAR_F16 ? launch_sample<f16>(a, n, st)
+                                        : launch_sample<bf16>(a, n, st);
 }

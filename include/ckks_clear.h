@@ -110,7 +110,8 @@ int ckks_clear_cache_append(const ckks_clear_append_t *a, void *stream);
  * A query that sees no key (or only keys with scores of -infinity) gets out = 0 and lse = -infinity.  Keys and values that a query
  * does not see do not reach its result, whatever they hold.  A page outside [0, n_pages) reads as zeros.  scale > 0 and finite,
  * scores scale q.k and their multiples by log2(e) within the range of 32 bits.  Rows of q in no sequence are not written.
- * heads: a multiple of kv_heads, at most 65536, n_tokens * heads / kv_heads below 2^31.
+ * heads: a multiple of kv_heads, at most 65536, n_tokens * heads / kv_heads below 2^31.  One launch has to have a block of 256 threads or
+ * 512 for each tile of queries and kv head, so some 2^23 single tokens times kv heads are the most.
  * All sums are 32-bit.  With 16-bit types a weight of the softmax meets the values as a high and a low number of that type for
  * single tokens and short chunks: only the result is rounded to the type.  For chunks whose products fill the device, by the
  * measured costs of either way, it is rounded to the type: F16 with its 11 bits down to 2^-25 of the row's largest so far, to steps

@@ -960,10 +960,14 @@ static bool plan_attend(const AttendSizes &p, AttendPlan &n) {
         const AttendForm &form = f < count ? forms[f] : *p.thin;
         if (p.thin && f < count && (f32 || form.waves_rows == 1)) continue;  // what it takes the place of
         const double blocks = (seqs ? seqs * std::ceil(per_seq / form.rows) : 1) * g.kv_heads;
-        const bool may_split = (u64)b.n_tokens * p.heads < 1u << 31;  // the joining kernel's grid
-        const double most = !may_split ? 1.0 : std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));
+        // a launch has fewer than 2^32 threads, the joining kernel's too
+        const u64 threads = (rows / form.rows + seqs) * g.kv_heads * (form.waves_rows == 8 ? 512 : 256), joined = (u64)b.n_tokens * p.heads;
+        const auto fits = [&](u32 splits) {
+            return threads * splits < 1ull << 32 && (splits == 1 || joined * (splits <= 8 ? 64 : splits <= 32 ? 256 : 1024) < 1ull << 32);
+        };
+        const double most = std::max(1.0, std::min(1024.0, keys / form.keys / (form.waves_rows > 1 ? 4 : 1)));
         auto consider = [&](u32 splits) {
-            if (splits < 1 || splits > most) return;
+            if (splits < 1 || splits > most || !fits(splits)) return;
             const double load = blocks * splits / CUS, steps = std::ceil(keys / splits / form.keys);
             const double share = form.fit > 1 ? std::min(1.0, std::max(0.0, (load - 1) / (form.fit - 1))) : 0.0;
             const double step = form.step_us + share * (form.full_us - form.step_us), rounds = load / form.fit;
@@ -984,9 +988,8 @@ static bool plan_attend(const AttendSizes &p, AttendPlan &n) {
         for (u32 splits = 1; splits <= most; splits += std::max(1u, splits / 2)) consider(splits);
         for (u32 k = 1; k <= 2; ++k) consider((u32)std::min(1024.0, k * CUS / blocks));  // as many blocks as CUs, or twice that
     }
-    const u64 tiles = rows / n.form.rows + seqs;  // at most
-    if (tiles * g.kv_heads * n.splits >= 1u << 31) return false;
-    n.tiles = (u32)tiles;
+    if (!n.splits) return false;
+    n.tiles = (u32)(rows / n.form.rows + seqs);  // at most
     n.min_tiles = 4;
     n.work_bytes = n.splits > 1 ? (u64)n.splits * b.n_tokens * p.heads * (g.head_dim + 1) * 4 : 0;
     return true;

@@ -230,7 +230,19 @@ template <class T, class TO, int THREADS, int R, bool RULES>
 static void launch_logits(LogitsArgs a, u32 rows, hipStream_t st) {
     constexpr u32 span = THREADS * 8 * R;
     a.tiles = (a.vocab + span - 1) / span;
-    hipLaunchKernelGGL((logits_kernel<T, TO, THREADS, R, RULES>), dim3(rows * a.tiles), dim3(THREADS), 0, st, a);
+    // a launch has fewer than 2^32 threads: its rows, and on to the next ones
+    const u32 most = std::max(((1u << 21) - 1) / a.tiles, 1u);
+    for (u32 n; rows; rows -= n) {
+        n = std::min(rows, most);
+        hipLaunchKernelGGL((logits_kernel<T, TO, THREADS, R, RULES>), dim3(n * a.tiles), dim3(THREADS), 0, st, a);
+        a.logits = (const T *)a.logits + (i64)n * a.ls;
+        a.out = (TO *)a.out + (i64)n * a.os;
+        for (const int32_t **p : {&a.token_start, &a.n_prompt, &a.bias_start})
+            if (*p) *p += n;
+        for (const float **p : {&a.repetition, &a.frequency, &a.presence})
+            if (*p) *p += n;
+        if (a.mask) a.mask += (i64)n * a.ms;
+    }
 }
 // Stretches: each block goes through the row's whole history, so long ones go through it less often, short ones put more CUs to
 // work.  Measured on one card, history of h tokens a row, us:

@@ -47,7 +47,7 @@ int ckks_clear_layer_norm(const ckks_clear_norm_t *a, void *stream);
 /* Gradient: with xh = (x - mean) rstd and g = dy * weight,
  *   dx = rstd (g - mean(g) - xh mean(g xh)),  dweight = sum over rows of dy xh,  dbias = sum over rows of dy.
  * d_dx [rows] by dx_stride, may be d_dy with the same stride; or NULL.  d_dweight, d_dbias [cols] of weight_dtype, either NULL;
- * zeros for rows = 0.  Row sums are joined in a fixed order: the same inputs give the same bits.
+ * zeros for rows = 0.  Row sums are joined in a fixed order: the same inputs give the same bits; cols below 2^28 for either.
  * d_work: at least ckks_clear_layer_norm_grad_work_bytes(rows, cols, dtype) bytes, 4-byte aligned, contents free;
  * may be NULL when both d_dweight and d_dbias are. */
 typedef struct {

@@ -528,6 +528,10 @@ int ckks_clear_layer_norm_grad(const ckks_clear_norm_grad_t *p, void *stream) {
     if (int rc = check_norm("ckks_clear_layer_norm_grad", p->rows, p->cols, p->dtype, p->weight_dtype)) return rc;
     const u32 dtype = p->dtype, wtype = p->weight_dtype, e = clear_dtype_bytes(dtype), we = clear_dtype_bytes(wtype);
     const bool params = p->d_dweight || p->d_dbias;
+    if (params && p->cols >= 1u << 28) {  // 16 threads to a column where row sums are joined, and fewer than 2^32 in a launch
+        set_error("ckks_clear_layer_norm_grad: gradients of %u weights exceed one launch", p->cols);
+        return CKKS_E_INVAL;
+    }
     const u64 need = params ? ckks_clear_layer_norm_grad_work_bytes(p->rows, p->cols, dtype) : 0;
     if (need > p->work_bytes || (need && (!p->d_work || (uintptr_t)p->d_work % 4))) {
         set_error("ckks_clear_layer_norm_grad: workspace of %llu bytes, needs %llu (4-byte aligned)", (unsigned long long)p->work_bytes,

@@ -201,7 +201,7 @@ typedef struct {
 int ckks_clear_packed_append(const ckks_clear_packed_append_t *a, void *stream);
 
 /* Attention of the new tokens over the packed pages, in every respect as ckks_clear_attend over pages that hold, in dtype, what the
- * codes stand for (beyond its range F16 is infinite, as a conversion is). */
+ * codes stand for (beyond its range F16 is infinite, as a conversion is; numbers below 2^-126 may count as 0). */
 typedef struct {
     ckks_clear_packed_t pages;
     ckks_clear_batch_t batch;
@@ -244,7 +244,7 @@ int ckks_clear_packed_read(const ckks_clear_packed_read_t *a, void *stream);
  * counts as 0, u of 1 or more takes the last token kept; NaN counts as no limit, temperature 1, u = 0.
  * A logit of -infinity or NaN is never drawn, and one whose w is below 2^-64 counts as -infinity; logits of +infinity are drawn alike.
  * A row without any other gets token -1, prob 0.  Sums are held in 64 bits, off by less than 2^-40 of themselves, and joined in a fixed
- * order: the same inputs give the same token.  d_prob: f32 [rows] or NULL. */
+ * order: the same inputs give the same token.  d_prob: f32 [rows] or NULL.  vocab: 1 to 2^20, rows below 2^31. */
 typedef struct {
     const void *d_logits;
     int32_t *d_token;

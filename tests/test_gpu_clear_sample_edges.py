@@ -67,3 +67,21 @@ def test_the_first_and_the_last_token_kept_may_weigh_little(vocab, dtype):
             args = {k: torch.tensor(v, device="cuda", dtype=torch.int32 if k == "top_k" else torch.float32) for k, v in more.items()}
             assert K.ckks_clear_sample(logits, torch.full((3,), u, device="cuda"), **args).tolist() == list(at)
 
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_that_a_mask_leaves_empty_or_with_one_token(dtype):
+    """-1 for a row of -infinity or NaN alone, whatever the limits and the temperature; the one token that is left, or that outweighs all."""
+    low = torch.finfo(TYPES[dtype]).min
+    logits = torch.full((4, 5000), -math.inf, device="cuda", dtype=TYPES[dtype])
+    logits[1] = math.nan
+    logits[2] = low
+    logits[2, 77] = 0.5
+    logits[3, 4321] = low
+    for u in (0.0, 0.5, 1.0):
+        for temperature in (1.0, 0.0, 5.0, math.inf, math.nan):
+            for more in ({}, {"top_k": 5}, {"top_k": 900}, {"top_p": 0.6}, {"min_p": 0.2}, {"top_k": 100, "top_p": 0.9}):
+                got = check(logits, [u] * 4, temperature=[temperature] * 4, **{k: [x] * 4 for k, x in more.items()}).tolist()
+                assert got[:2] == [-1, -1]
+                assert got[3] == 4321
+                assert got[2] == 77 or temperature == math.inf

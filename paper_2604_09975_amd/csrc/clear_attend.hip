@@ -19,7 +19,7 @@
 //   1 token over 131002 keys, 16 and 2 heads, KW = 4, split: 26 to 30 us and 5 us to join (134 MB, 27 us at a copy's rate);
 //   1 token over 128 keys, 12 heads of 64: 6.9 us; 128 tokens of 32 bits: 10.7 us: the chain of lookup, load, product, join.
 //   Heads of 136 to 256 do not fit the registers: 107 of a lane lie in scratch with KW = 4 (64 tokens over 8192 keys, 8 heads of 256, bf16
-//     1.22 ms, 3.5 TB/s; one token 36 us), 34 with RW = 4 in 32 bits (92 TFLOP/s); RW = 4 in 16 bits reaches 590 TFLOP/s.
+//     1.22 ms, 3.5 TB/s; one token 36 us), 34 with RW = 4 in 32 bits (94 TFLOP/s); RW = 4 in 16 bits reaches 590 TFLOP/s.
 #include "clear_attend_device.h"
 
 using namespace ckks;

@@ -1,7 +1,9 @@
 // Attention over pages of 8 bits.  Chunks go through the kernels of clear_attend.hip: codes are brought to the queries' type, exactly, on
 // their way into LDS, and from there on nothing differs.  Few rows over heads of up to 128 have a kernel of their own.
 // Chunks are bound by the matrix products and, between them, by what a weight costs: 2 x 4096 tokens of 32 heads of 128 over up to 12301
-// keys take 1370 to 1490 us with E4M3 (890 TF), 1655 with I8, 1300 over a plain bf16 cache.
+// keys take 1370 to 1490 us with E4M3 (0.96 to 0.89 PFLOP/s), 1540 to 1655 with I8, 1300 over a plain bf16 cache.  Their weights are rounded to the type
+// before the second product, as there and for the same reason: the error against 64 bits is 0.0021 of the result where one rounding of
+// it alone gives 0.0017.
 #include "clear_attend_device.h"
 
 namespace ckks {
@@ -11,7 +13,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// What codes become in the matrix products over few rows: F16 for F16, else BF16, which holds every code times a power of two.  A 32-bit
+// What codes become in the matrix products over few rows: F16 for F16, else BF16, which holds every code times a power of two down to 2^-133.  A 32-bit
 // number goes into them as three of 8 bits, a softmax weight of the 16-bit types as two.
 template <class T>
 struct Thin {
@@ -53,7 +55,8 @@ __device__ __forceinline__ float row_sum(float x) {
 // arithmetic; I8, whose codes take two instructions each to expand, 162.  attend_kernel's waves-apart form took 231 over a plain cache, of
 // twice the bytes.  One tile a wave is in flight at 3 waves a SIMD: with two at 2 waves 156 us where this took 146, at 4 waves
 // registers spill (169).  One sequence of 131001 keys (2 heads of 128, 69 MB) is bound by its start, the joining launch and the
-// waves' last tiles: 24 us and 5 where the bytes take 14.
+// waves' last tiles: 24 us and 5 where the bytes take 14.  (One wave on a SIMD waits for each of its eight tiles; two tiles under way have not been
+// measured there.)
 // WHOLE: pages hold whole tiles.
 template <class T, int FORM, int DP, bool WHOLE, int KW, int OCC>
 __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendArgs a) {
@@ -462,7 +465,8 @@ __global__ __launch_bounds__(64 * KW, OCC) void attend_thin_kernel(PackedAttendA
 using namespace ckks;
 
 // attend_thin_kernel, as a form of plan_attend: by its costs few rows of 16-entry pieces and every F32 head come here, chunks of the
-// 16-bit types go to the forms whose waves share tiles.  F32 over 2 x 1024 tokens, 2000 keys each: 245 us here, 775 over a plain cache.
+// 16-bit types go to the forms whose waves share tiles.  F32, 2 x 1024 tokens over 2000 more keys, 32 / 8 heads of 128: 340 us here with E4M3, 456
+// with I8, 787 over a plain cache.
 constexpr AttendForm THIN_64 = {0, 16, 32, 128, 5, 0.8f, 1.2f, 3}, THIN_128 = {0, 16, 32, 128, 5, 1.0f, 2.0f, 3};
 
 static AttendSizes sizes(const ckks_clear_packed_attend_t &p) {

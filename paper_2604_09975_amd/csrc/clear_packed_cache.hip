@@ -8,8 +8,8 @@
 // exact products, worked out once for all heads of the token, and r = 1/sqrt(mean(x^2) + eps).  Of the 53 bits the upper 21 go on,
 // the last of them set if anything below is (round to odd): rounding that to a type of 19 bits or fewer rounds once.
 //
-// Many tokens are bound by memory: 22600 tokens of 32 heads and 8 kv heads of 128 in bf16, normed and rotated, take 127 us (512 MB, 4.0
-// TB/s), 112 without norm and rotation (4.6), F32 into I8 195 (5.0).  A few tokens are bound by one wave's way through place, angles
+// Many tokens are bound by memory: 22600 tokens of 32 heads and 8 kv heads of 128 in bf16, normed and rotated, take 128 us (512 MB, 4.0
+// TB/s), 111 without norm and rotation (4.6), F32 into I8 195 (5.0).  A few tokens are bound by one wave's way through place, angles
 // and sum (3.7 us), so there each turn of a token's work has a wave of its own.  Weights go through LDS (the block's tokens share them)
 // and the first rows are loaded after them: with those loads ahead of the weights 143 us instead of 128, in scalar loads 158.
 #include <algorithm>

@@ -16,8 +16,9 @@
 // The draw sums the kept weights by stretches of ids and looks into the one that holds u.
 //
 // Bound by a weight's 25 instructions or so in 64 bits where each row has a CU, not by the logits' bytes: 256 rows of 131072 bf16 (67 MB,
-// 14 us by the bytes) take 37 us with no limit, 33 with top_k 50, which needs no weights but the list's, 129 with top_p 0.9, which needs
-// all of them and a border resolved.  A single row has one CU: 50257 logits 13.8 us with a list, 40 with top_p 0.9 alone.
+// 14 us by the bytes) take 44 us with no limit, 29 with top_k 50, which needs no weights but the list's, 116 with top_p 0.9, which needs
+// all of them and a border resolved.  A single row has one CU: 50257 logits 14 us with a list, 42 with top_p 0.9 alone.
+// 1024 threads leave 128 registers each: of F32 rows 10 lie in scratch, at the edges of the steps, of 16-bit ones none.
 #include <algorithm>
 #include <type_traits>
 

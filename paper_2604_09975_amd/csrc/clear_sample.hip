@@ -82,14 +82,14 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a) {
     constexpr int PER = BINS / THREADS;
     constexpr u32 APART = THREADS == 1024 ? 8192 : 2048;
     constexpr u32 SPAN = THREADS * V, WAVES = THREADS / 64;    // SPAN: ids of a round
-    __shared__ __attribute__((aligned(16))) u64 mass[CHUNKS];  // weights of the bins; of stretches of ids (64-bit floats); lists
+    __shared__ __attribute__((aligned(16))) u64 mass[CHUNKS];  // weights of the bins, as whole numbers; of stretches of ids; lists
     __shared__ u32 count[CHUNKS];                              // tokens of the bins; of stretches of ids that have the last value
     __shared__ u64 apart[APART];                               // tokens set apart, those that all later passes are about
     __shared__ double power[GRAIN];                            // 2^(j / 256)
     __shared__ u32 wave_counts[WAVES];
     __shared__ double wave_sums[WAVES];
     __shared__ u32 n_list, n_bin, key_min, key_max;
-    __shared__ u32 found[4], found_count;
+    __shared__ u32 found[3], found_count;
     __shared__ double found_sum;
     __shared__ float wave_top[WAVES];
 
